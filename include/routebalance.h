@@ -46,17 +46,20 @@ typedef enum {
     RB_OK = 0,
     RB_ERR_NULL = -1,        /* a required pointer is NULL */
     RB_ERR_DIMS = -2,        /* a size is out of range (see each call) */
-    RB_ERR_DTYPE = -3,       /* dtype is not RB_F32 or RB_BF16 */
+    RB_ERR_DTYPE = -3,       /* a dtype that the call does not take */
     RB_ERR_WEIGHTS = -4,     /* weights not finite, negative, or |sum - 1| > 1e-5 */
-    RB_ERR_WORKSPACE = -5,   /* workspace NULL or smaller than rb_workspace_size */
+    RB_ERR_WORKSPACE = -5,   /* workspace NULL or smaller than its *_workspace_size */
     RB_ERR_UNSUPPORTED = -6, /* an option this version does not implement */
     RB_ERR_HIP = -7,         /* a HIP runtime call or kernel launch failed */
     RB_ERR_ALIGN = -8,       /* a pointer is not aligned as required */
-    RB_ERR_SCRATCH = -9      /* rb_route_batch_noalloc: these sizes need more workspace than
+    RB_ERR_SCRATCH = -9,     /* rb_route_batch_noalloc: these sizes need more workspace than
                                 RB_SCRATCH_BYTES */
+    RB_ERR_VALUE = -10       /* a scalar argument (beta, decay, usage0) is out of range */
 } rb_status;
 
-typedef enum { RB_F32 = 0, RB_BF16 = 1 } rb_dtype;
+/* RB_Q4 is taken by rb_attend, rb_attend_usage and rb_bank_replace only: rows
+ * held in 4 bits as rb_bank_pack writes them, with queries in bf16. */
+typedef enum { RB_F32 = 0, RB_BF16 = 1, RB_Q4 = 2 } rb_dtype;
 
 /* Neighbour-averaging rule (Sec. 4.2 calls the paper's KNN "distance-weighted"
  * without giving the weights).
@@ -367,6 +370,126 @@ rb_status rb_route_batch_noalloc(const void *queries, const void *bank, const fl
                                  rb_weights w, int32_t *assign, float *chosen_score,
                                  int32_t *nbr_idx, float *nbr_dist, float *q_hat, float *l_hat,
                                  float *score0, void *stream);
+
+/* ---- Attention over the labelled bank --------------------------------------
+ *
+ * The calls above predict from the k nearest rows. These weigh every row: request
+ * b gives row n the weight
+ *   p[b][n] = exp(-beta * |q_b - x_n|^2) / sum_j exp(-beta * |q_b - x_j|^2)
+ * (a softmax over the negated squared distances, j over the rows whose mask is
+ * not 0), which is smooth in the requests, the rows, the labels and beta, so that
+ * all four can be trained. Distances as in rb_knn_topk (fp32 products and
+ * accumulation); the maximum of the softmax is subtracted, so no weight
+ * overflows. Arguments shared by the calls:
+ *   queries   [B][d] of dtype (bf16 for RB_Q4), 16-byte aligned.
+ *   bank      RB_F32, RB_BF16: [N][d]; RB_Q4: [N][d/2] bytes (rb_bank_pack);
+ *             16-byte aligned.
+ *   scales    RB_Q4: [N][d/32] bytes; otherwise not read and may be NULL.
+ *   bank_norms [N] fp32, from rb_bank_norms (RB_Q4: rb_bank_pack).
+ *   beta      sharpness, 1e-30 <= beta <= 1e30.
+ *   row_mask  [N] uint8 or NULL: rows whose mask is 0 take no part, whatever
+ *             they, their norms and their labels hold (numbers or not).
+ *   ws        device workspace of ws_bytes >= the call's *_workspace_size,
+ *             256-byte aligned; its contents on entry do not matter, and calls
+ *             that may overlap need workspaces of their own.
+ * A request whose every row is masked has no weights: its predictions are NaN,
+ * its lse -inf, and it adds nothing to any gradient or usage.
+ * Results are deterministic (sums in a fixed order, no floating atomics). B = 0
+ * enqueues nothing but (rb_attend_usage) the decay and (rb_attend_backward) the
+ * zeros of the gradients of the bank.
+ * Errors shared by the calls: RB_ERR_DTYPE; RB_ERR_DIMS (B < 0, N < 1, d < 1,
+ * d > RB_MAX_D, d not a multiple of 4 for RB_F32, 8 for RB_BF16, 32 for RB_Q4,
+ * M < 1, M > RB_MAX_M); RB_ERR_VALUE; RB_ERR_NULL; RB_ERR_ALIGN; RB_ERR_WORKSPACE;
+ * RB_ERR_HIP. The *_workspace_size calls write the bytes for these sizes on the
+ * current device to *bytes (a host pointer). */
+
+/* Predictions: q_hat[b][m] = sum_n p[b][n] * bank_qual[n][m], l_hat likewise from
+ * bank_len, and lse[b] = log(sum_n exp(-beta*|q_b - x_n|^2)).
+ *   bank_qual, bank_len [N][M] fp32; q_hat, l_hat [B][M] fp32 (outputs);
+ *   lse [B] fp32 (output, may be NULL). The outputs can go to rb_score and
+ *   rb_assign as those of rb_knn_predict do.
+ * Sums, maxima and weights are fp32. */
+rb_status rb_attend_workspace_size(int B, int N, int d, rb_dtype dtype, int M, size_t *bytes);
+rb_status rb_attend(const void *queries, const void *bank, const uint8_t *scales,
+                    const float *bank_norms, rb_dtype dtype, int B, int N, int d, float beta,
+                    const uint8_t *row_mask, const float *bank_qual, const float *bank_len, int M,
+                    float *q_hat, float *l_hat, float *lse, void *ws, size_t ws_bytes,
+                    void *stream);
+
+/* Gradients of rb_attend, whose probabilities are recomputed from lse. With
+ * dq_hat, dl_hat [B][M] and dlse [B] (may be NULL: 0) the gradients of its
+ * outputs, and q_hat, l_hat, lse its outputs for the same inputs:
+ *   ds[b][n]  = p[b][n] * (sum_m dq_hat[b][m]*(bank_qual[n][m] - q_hat[b][m])
+ *                        + sum_m dl_hat[b][m]*(bank_len[n][m] - l_hat[b][m]) + dlse[b])
+ *   d_queries[b] = 2*beta * sum_n ds[b][n]*(x_n - q_b)     [B][d] of dtype
+ *   d_bank[n]    = 2*beta * sum_b ds[b][n]*(q_b - x_n)     [N][d] of dtype
+ *   d_qual[n]    = sum_b p[b][n]*dq_hat[b]                 [N][M] fp32, d_len likewise
+ *   d_beta[b]    = -sum_n ds[b][n]*|q_b - x_n|^2           [B] fp32 (the gradient of
+ *                  beta is their sum)
+ * Each of the five outputs may be NULL and is then not computed; masked rows get
+ * gradients of 0. Outputs are overwritten, and must not overlap the inputs. The
+ * norms are taken as functions of the rows. dtype is RB_F32 or RB_BF16. For
+ * bf16, ds enters the two products over d as a sum of two bf16 values (17 bits).
+ * d_queries, d_bank 16-byte aligned. */
+rb_status rb_attend_backward_workspace_size(int B, int N, int d, rb_dtype dtype, int M,
+                                            size_t *bytes);
+rb_status rb_attend_backward(const void *queries, const void *bank, const float *bank_norms,
+                             rb_dtype dtype, int B, int N, int d, float beta,
+                             const uint8_t *row_mask, const float *bank_qual,
+                             const float *bank_len, int M, const float *q_hat, const float *l_hat,
+                             const float *lse, const float *dq_hat, const float *dl_hat,
+                             const float *dlse, void *d_queries, void *d_bank, float *d_qual,
+                             float *d_len, float *d_beta, void *ws, size_t ws_bytes,
+                             void *stream);
+
+/* Weight that a batch gives each row, accumulated from batch to batch:
+ *   usage[n] = decay * usage[n] + sum_b p[b][n]            [N] fp32, in place
+ * with lse [B] from rb_attend for the same inputs; 0 <= decay <= 1 (with 0 the
+ * old contents, finite, do not matter). Masked rows only decay. */
+rb_status rb_attend_usage_workspace_size(int B, int N, int d, rb_dtype dtype, size_t *bytes);
+rb_status rb_attend_usage(const void *queries, const void *bank, const uint8_t *scales,
+                          const float *bank_norms, rb_dtype dtype, int B, int N, int d, float beta,
+                          const uint8_t *row_mask, const float *lse, float decay, float *usage,
+                          void *ws, size_t ws_bytes, void *stream);
+
+/* Holds a bank in 4 bits: every 32 elements of a row share a scale 2^(s - 127),
+ * the least power of two (s >= 1) under which none of them passes 6, and an
+ * element is the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0 to 7, ties to the
+ * even code) times it, bit 3 of the code its sign. A byte holds two elements, the
+ * even one in its low half.
+ *   bank [N][d] of dtype (RB_F32 or RB_BF16, finite), 16-byte aligned;
+ *   d a multiple of 32; rows [N][d/2], 16-byte aligned, scales [N][d/32], norms
+ *   [N] fp32 of the values held (outputs).
+ * Errors: RB_ERR_NULL, RB_ERR_DTYPE, RB_ERR_DIMS, RB_ERR_ALIGN, RB_ERR_HIP. */
+rb_status rb_bank_pack(const void *bank, rb_dtype dtype, int N, int d, uint8_t *rows,
+                       uint8_t *scales, float *norms, void *stream);
+
+/* Rows to make room: the n rows of least usage among those whose may_go is not 0
+ * (NULL: all), equal usage (0 and -0 are equal) by the lower row first, NaN last.
+ *   usage [N] fp32; may_go [N] uint8 or NULL; victims [n] int32 (output): row
+ *   indices ascending, -1 behind them if fewer than n rows may go.
+ * n = 0 enqueues nothing. Errors: RB_ERR_DIMS (N < 1, n < 0, n > N), RB_ERR_NULL,
+ * RB_ERR_WORKSPACE, RB_ERR_ALIGN (ws), RB_ERR_HIP. */
+rb_status rb_evict_workspace_size(int N, size_t *bytes);
+rb_status rb_bank_evict(const float *usage, const uint8_t *may_go, int N, int n, int32_t *victims,
+                        void *ws, size_t ws_bytes, void *stream);
+
+/* New rows in place of old ones: row at[j] of the bank becomes new_rows[j], with
+ * its norm, labels and, where usage is not NULL, usage0 as its usage; entries of
+ * at outside [0, N) are passed over. The entries inside are distinct
+ * (a precondition). Rows not named stay as they are.
+ *   at [n] int32; new_rows [n][d] of src_dtype, 16-byte aligned, which is dtype,
+ *   or for a bank of RB_Q4 RB_F32 or RB_BF16 (held in 4 bits as by rb_bank_pack);
+ *   new_qual, new_len [n][M] fp32; bank, scales, bank_norms, bank_qual, bank_len,
+ *   usage as above, in place; usage0 finite.
+ * A row's norm is bit for bit the one rb_bank_norms or rb_bank_pack gives.
+ * n = 0 enqueues nothing. Errors: RB_ERR_DTYPE, RB_ERR_DIMS (N < 1, n < 0, d as
+ * above, M < 1, M > RB_MAX_M), RB_ERR_VALUE, RB_ERR_NULL, RB_ERR_ALIGN, RB_ERR_HIP. */
+rb_status rb_bank_replace(const int32_t *at, int n, const void *new_rows, rb_dtype src_dtype,
+                          const float *new_qual, const float *new_len, int M, void *bank,
+                          uint8_t *scales, float *bank_norms, rb_dtype dtype, int N, int d,
+                          float *bank_qual, float *bank_len, float *usage, float usage0,
+                          void *stream);
 
 /* Carry the dead-reckoned state across a gap of dt_seconds between batches:
  *   prefill_q[i] = max(0, prefill_q[i] - prefill_rate[i]*dt)

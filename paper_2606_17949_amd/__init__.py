@@ -10,6 +10,7 @@ library has not been built (``python -m paper_2606_17949_amd.build``).
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import dataclasses
 import os
@@ -22,7 +23,8 @@ LIB_PATH = os.path.join(_HERE, "librouteb.so")
 
 RB_OK, RB_ERR_NULL, RB_ERR_DIMS, RB_ERR_DTYPE, RB_ERR_WEIGHTS = 0, -1, -2, -3, -4
 RB_ERR_WORKSPACE, RB_ERR_UNSUPPORTED, RB_ERR_HIP, RB_ERR_ALIGN, RB_ERR_SCRATCH = -5, -6, -7, -8, -9
-RB_F32, RB_BF16 = 0, 1
+RB_ERR_VALUE = -10
+RB_F32, RB_BF16, RB_Q4 = 0, 1, 2
 RB_KNN_UNIFORM, RB_KNN_INV_DIST = 0, 1
 RB_ORDER_ARRIVAL, RB_ORDER_LPT = 0, 1
 RB_FLAG_OVERLAP, RB_FLAG_LISTS_ONLY, RB_FLAG_FROM_LISTS = 1, 2, 4
@@ -33,7 +35,10 @@ RB_SCRATCH_BYTES = 64 << 20
 EXPORTS = ("rb_status_string", "rb_workspace_size", "rb_bank_norms", "rb_knn_topk", "rb_predict",
            "rb_score", "rb_assign", "rb_assign_ex", "rb_knn_predict", "rb_route_batch",
            "rb_route_batch_ex", "rb_advance_state", "rb_profile_scan_events",
-           "rb_route_batch_noalloc")
+           "rb_route_batch_noalloc", "rb_attend_workspace_size", "rb_attend",
+           "rb_attend_backward_workspace_size", "rb_attend_backward",
+           "rb_attend_usage_workspace_size", "rb_attend_usage", "rb_bank_pack",
+           "rb_evict_workspace_size", "rb_bank_evict", "rb_bank_replace")
 
 
 class RbError(RuntimeError):
@@ -64,7 +69,7 @@ def _load():
         raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_2606_17949_amd.build`")
     lib = ctypes.CDLL(LIB_PATH)
     P, i, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
-    st = ctypes.c_int
+    st, f32 = ctypes.c_int, ctypes.c_float
     sig = {
         "rb_status_string": ([st], ctypes.c_char_p),
         "rb_workspace_size": ([i, i, i, i, i, i, ctypes.POINTER(sz)], st),
@@ -88,6 +93,17 @@ def _load():
                                     P, P, P], st),
         "rb_advance_state": ([ctypes.POINTER(rb_instances), i, ctypes.c_float, P], st),
         "rb_profile_scan_events": ([P, P], st),
+        "rb_attend_workspace_size": ([i, i, i, i, i, ctypes.POINTER(sz)], st),
+        "rb_attend": ([P, P, P, P, i, i, i, i, f32, P, P, P, i, P, P, P, P, sz, P], st),
+        "rb_attend_backward_workspace_size": ([i, i, i, i, i, ctypes.POINTER(sz)], st),
+        "rb_attend_backward": ([P, P, P, i, i, i, i, f32, P, P, P, i, P, P, P, P, P, P, P, P, P, P,
+                                P, P, sz, P], st),
+        "rb_attend_usage_workspace_size": ([i, i, i, i, ctypes.POINTER(sz)], st),
+        "rb_attend_usage": ([P, P, P, P, i, i, i, i, f32, P, P, f32, P, P, sz, P], st),
+        "rb_bank_pack": ([P, i, i, i, P, P, P, P], st),
+        "rb_evict_workspace_size": ([i, ctypes.POINTER(sz)], st),
+        "rb_bank_evict": ([P, P, i, i, P, P, sz, P], st),
+        "rb_bank_replace": ([P, i, P, i, P, P, i, P, P, P, i, i, i, P, P, P, f32, P], st),
     }
     for name, (args, res) in sig.items():
         f = getattr(lib, name)
@@ -544,3 +560,283 @@ def rb_profile_scan_events(begin=None, end=None):
     b = ctypes.c_void_p(begin.cuda_event) if begin is not None else None
     e = ctypes.c_void_p(end.cuda_event) if end is not None else None
     _check(_lib.rb_profile_scan_events(b, e), "rb_profile_scan_events")
+
+
+# ---- attention over the labelled bank
+
+
+def _one_device(dev: torch.device, **tensors):
+    """Every tensor on ``dev`` (an address of another GPU would fault)."""
+    for name, t in tensors.items():
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name}: on {t.device}, the queries or the bank on {dev}")
+
+
+def _on(dev: torch.device):
+    """Makes ``dev`` current for the call (a no-op where it is)."""
+    if dev.type != "cuda" or dev.index in (None, torch.cuda.current_device()):
+        return contextlib.nullcontext()
+    return torch.cuda.device(dev)
+
+
+def _bank(bank, bank_norms, scales, row_mask):
+    """(code, N, d) of a bank of fp32, bf16 or 4-bit rows (uint8 [N][d/2], with
+    scales [N][d/32])."""
+    if not isinstance(bank, torch.Tensor) or bank.dim() != 2:
+        raise ValueError("bank: expected a 2-d tensor")
+    N, d = (int(x) for x in bank.shape)
+    if bank.dtype == torch.uint8:
+        code, d = RB_Q4, 2 * d
+        if scales is None:
+            raise ValueError("scales: a bank held in 4 bits needs them")
+        _expect(scales, torch.uint8, (N, d // 32), "scales")
+    else:
+        code = _embedding_code(bank, "bank")
+        if scales is not None:
+            raise ValueError("scales: only for a bank held in 4 bits (uint8)")
+    _expect(bank_norms, torch.float32, (N,), "bank_norms")
+    _expect_opt(row_mask, torch.uint8, (N,), "row_mask")
+    return code, N, d
+
+
+def _embedding_code(t, name):
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"{name}: unsupported embedding dtype {t.dtype}")
+    return _dtype_code(t)
+
+
+def _attend_queries(queries, code, d):
+    """B of the queries of a bank (bf16 for 4-bit rows)."""
+    if not isinstance(queries, torch.Tensor) or queries.dim() != 2:
+        raise ValueError("queries: expected a 2-d tensor")
+    B = int(queries.shape[0])
+    _expect(queries, torch.float32 if code == RB_F32 else torch.bfloat16, (B, d), "queries")
+    return B
+
+
+def _size(fn, *args) -> int:
+    n = ctypes.c_size_t(0)
+    _check(getattr(_lib, fn)(*args, ctypes.byref(n)), fn)
+    return int(n.value)
+
+
+def _buffer(n: int, device) -> torch.Tensor:
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def rb_attend_workspace_size(B: int, N: int, d: int, dtype: int, M: int) -> int:
+    return _size("rb_attend_workspace_size", B, N, d, dtype, M)
+
+
+def rb_attend_backward_workspace_size(B: int, N: int, d: int, dtype: int, M: int) -> int:
+    return _size("rb_attend_backward_workspace_size", B, N, d, dtype, M)
+
+
+def rb_attend_usage_workspace_size(B: int, N: int, d: int, dtype: int) -> int:
+    return _size("rb_attend_usage_workspace_size", B, N, d, dtype)
+
+
+def rb_evict_workspace_size(N: int) -> int:
+    return _size("rb_evict_workspace_size", N)
+
+
+def attend_workspace(B: int, N: int, d: int, dtype: int, M: int, device="cuda") -> torch.Tensor:
+    """A device workspace of the size rb_attend_workspace_size asks for."""
+    return _buffer(rb_attend_workspace_size(B, N, d, dtype, M), device)
+
+
+def attend_backward_workspace(B: int, N: int, d: int, dtype: int, M: int,
+                              device="cuda") -> torch.Tensor:
+    """A device workspace of the size rb_attend_backward_workspace_size asks for."""
+    return _buffer(rb_attend_backward_workspace_size(B, N, d, dtype, M), device)
+
+
+def attend_usage_workspace(B: int, N: int, d: int, dtype: int, device="cuda") -> torch.Tensor:
+    """A device workspace of the size rb_attend_usage_workspace_size asks for."""
+    return _buffer(rb_attend_usage_workspace_size(B, N, d, dtype), device)
+
+
+def evict_workspace(N: int, device="cuda") -> torch.Tensor:
+    """A device workspace of the size rb_evict_workspace_size asks for."""
+    return _buffer(rb_evict_workspace_size(N), device)
+
+
+def rb_attend(queries, bank, bank_norms, beta: float, bank_qual, bank_len,
+              scales: Optional[torch.Tensor] = None, row_mask: Optional[torch.Tensor] = None,
+              q_hat: Optional[torch.Tensor] = None, l_hat: Optional[torch.Tensor] = None,
+              lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """Predictions (q_hat, l_hat [B][M]) under a softmax over every bank row, and
+    lse [B]. ``bank`` is fp32 or bf16 [N][d], or uint8 [N][d/2] with ``scales``."""
+    code, N, d = _bank(bank, bank_norms, scales, row_mask)
+    B = _attend_queries(queries, code, d)
+    M = _labels(bank_qual, bank_len, N)
+    for t, shape, name in ((q_hat, (B, M), "q_hat"), (l_hat, (B, M), "l_hat"), (lse, (B,), "lse")):
+        _expect_opt(t, torch.float32, shape, name)
+    if ws is not None:
+        _expect(ws, torch.uint8, (ws.numel(),), "ws")
+    dev = queries.device
+    _one_device(dev, bank=bank, bank_norms=bank_norms, bank_qual=bank_qual, bank_len=bank_len,
+                scales=scales, row_mask=row_mask, q_hat=q_hat, l_hat=l_hat, lse=lse, ws=ws)
+    with _on(dev):
+        if q_hat is None:
+            q_hat = torch.empty(B, M, dtype=torch.float32, device=dev)
+        if l_hat is None:
+            l_hat = torch.empty(B, M, dtype=torch.float32, device=dev)
+        if lse is None:
+            lse = torch.empty(B, dtype=torch.float32, device=dev)
+        if ws is None:
+            ws = attend_workspace(B, N, d, code, M, dev)
+        _check(_lib.rb_attend(_ptr(queries), _ptr(bank), _ptr(scales), _ptr(bank_norms), code, B, N,
+                              d, float(beta), _ptr(row_mask), _ptr(bank_qual), _ptr(bank_len), M,
+                              _ptr(q_hat), _ptr(l_hat), _ptr(lse), _ptr(ws), ws.numel(),
+                              _stream(stream)), "rb_attend")
+    return q_hat, l_hat, lse
+
+
+def rb_attend_backward(queries, bank, bank_norms, beta: float, bank_qual, bank_len, q_hat, l_hat,
+                       lse, dq_hat, dl_hat, dlse: Optional[torch.Tensor] = None,
+                       row_mask: Optional[torch.Tensor] = None,
+                       d_queries: Optional[torch.Tensor] = None,
+                       d_bank: Optional[torch.Tensor] = None,
+                       d_qual: Optional[torch.Tensor] = None,
+                       d_len: Optional[torch.Tensor] = None,
+                       d_beta: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                       stream=None):
+    """Gradients of :func:`rb_attend`, into those of the five output tensors that
+    are given; with none given, all five are made. Returns them in a dict."""
+    code, N, d = _bank(bank, bank_norms, None, row_mask)
+    B = _attend_queries(queries, code, d)
+    M = _labels(bank_qual, bank_len, N)
+    f32 = torch.float32
+    for t, shape, name in ((q_hat, (B, M), "q_hat"), (l_hat, (B, M), "l_hat"), (lse, (B,), "lse"),
+                           (dq_hat, (B, M), "dq_hat"), (dl_hat, (B, M), "dl_hat")):
+        _expect(t, f32, shape, name)
+    _expect_opt(dlse, f32, (B,), "dlse")
+    out = {"d_queries": (d_queries, bank.dtype, (B, d)), "d_bank": (d_bank, bank.dtype, (N, d)),
+           "d_qual": (d_qual, f32, (N, M)), "d_len": (d_len, f32, (N, M)),
+           "d_beta": (d_beta, f32, (B,))}
+    for name, (t, dt, shape) in out.items():
+        _expect_opt(t, dt, shape, name)
+    if ws is not None:
+        _expect(ws, torch.uint8, (ws.numel(),), "ws")
+    dev = queries.device
+    _one_device(dev, bank=bank, bank_norms=bank_norms, bank_qual=bank_qual, bank_len=bank_len,
+                row_mask=row_mask, q_hat=q_hat, l_hat=l_hat, lse=lse, dq_hat=dq_hat,
+                dl_hat=dl_hat, dlse=dlse, ws=ws, **{n: v[0] for n, v in out.items()})
+    with _on(dev):
+        made = all(v[0] is None for v in out.values())
+        res = {n: torch.empty(shape, dtype=dt, device=dev) if made else t
+               for n, (t, dt, shape) in out.items()}
+        if ws is None:
+            ws = attend_backward_workspace(B, N, d, code, M, dev)
+        _check(_lib.rb_attend_backward(
+            _ptr(queries), _ptr(bank), _ptr(bank_norms), code, B, N, d, float(beta),
+            _ptr(row_mask), _ptr(bank_qual), _ptr(bank_len), M, _ptr(q_hat), _ptr(l_hat),
+            _ptr(lse), _ptr(dq_hat), _ptr(dl_hat), _ptr(dlse), _ptr(res["d_queries"]),
+            _ptr(res["d_bank"]), _ptr(res["d_qual"]), _ptr(res["d_len"]), _ptr(res["d_beta"]),
+            _ptr(ws), ws.numel(), _stream(stream)), "rb_attend_backward")
+    return {n: t for n, t in res.items() if t is not None}
+
+
+def rb_attend_usage(queries, bank, bank_norms, beta: float, lse, usage, decay: float = 1.0,
+                    scales: Optional[torch.Tensor] = None,
+                    row_mask: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                    stream=None):
+    """usage [N] = decay * usage + the weight this batch gives each row, in place."""
+    code, N, d = _bank(bank, bank_norms, scales, row_mask)
+    B = _attend_queries(queries, code, d)
+    _expect(lse, torch.float32, (B,), "lse")
+    _expect(usage, torch.float32, (N,), "usage")
+    if ws is not None:
+        _expect(ws, torch.uint8, (ws.numel(),), "ws")
+    dev = queries.device
+    _one_device(dev, bank=bank, bank_norms=bank_norms, scales=scales, row_mask=row_mask, lse=lse,
+                usage=usage, ws=ws)
+    with _on(dev):
+        if ws is None:
+            ws = attend_usage_workspace(B, N, d, code, dev)
+        _check(_lib.rb_attend_usage(_ptr(queries), _ptr(bank), _ptr(scales), _ptr(bank_norms), code,
+                                    B, N, d, float(beta), _ptr(row_mask), _ptr(lse), float(decay),
+                                    _ptr(usage), _ptr(ws), ws.numel(), _stream(stream)),
+               "rb_attend_usage")
+    return usage
+
+
+def rb_bank_pack(bank, rows: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                 norms: Optional[torch.Tensor] = None, stream=None):
+    """(rows uint8 [N][d/2], scales uint8 [N][d/32], norms [N]) of a bank held in 4 bits."""
+    if not isinstance(bank, torch.Tensor) or bank.dim() != 2:
+        raise ValueError("bank: expected a 2-d tensor")
+    code = _embedding_code(bank, "bank")
+    N, d = (int(x) for x in bank.shape)
+    if d % 32:
+        raise ValueError(f"bank: rows of {d} elements, expected a multiple of 32")
+    dev = bank.device
+    _expect_opt(rows, torch.uint8, (N, d // 2), "rows")
+    _expect_opt(scales, torch.uint8, (N, d // 32), "scales")
+    _expect_opt(norms, torch.float32, (N,), "norms")
+    _one_device(dev, rows=rows, scales=scales, norms=norms)
+    with _on(dev):
+        if rows is None:
+            rows = torch.empty(N, d // 2, dtype=torch.uint8, device=dev)
+        if scales is None:
+            scales = torch.empty(N, d // 32, dtype=torch.uint8, device=dev)
+        if norms is None:
+            norms = torch.empty(N, dtype=torch.float32, device=dev)
+        _check(_lib.rb_bank_pack(_ptr(bank), code, N, d, _ptr(rows), _ptr(scales), _ptr(norms),
+                                 _stream(stream)), "rb_bank_pack")
+    return rows, scales, norms
+
+
+def rb_bank_evict(usage, n: int, may_go: Optional[torch.Tensor] = None,
+                  victims: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                  stream=None):
+    """The n rows of least usage among those whose ``may_go`` is not 0: int32 [n],
+    ascending, -1 behind them if fewer may go."""
+    if not isinstance(usage, torch.Tensor) or usage.dim() != 1:
+        raise ValueError("usage: expected a 1-d tensor")
+    N = int(usage.shape[0])
+    _expect(usage, torch.float32, (N,), "usage")
+    _expect_opt(may_go, torch.uint8, (N,), "may_go")
+    _expect_opt(victims, torch.int32, (n,), "victims")
+    if ws is not None:
+        _expect(ws, torch.uint8, (ws.numel(),), "ws")
+    dev = usage.device
+    _one_device(dev, may_go=may_go, victims=victims, ws=ws)
+    with _on(dev):
+        if victims is None:
+            victims = torch.empty(max(n, 0), dtype=torch.int32, device=dev)
+        if ws is None:
+            ws = evict_workspace(N, dev)
+        _check(_lib.rb_bank_evict(_ptr(usage), _ptr(may_go), N, int(n), _ptr(victims), _ptr(ws),
+                                  ws.numel(), _stream(stream)), "rb_bank_evict")
+    return victims
+
+
+def rb_bank_replace(at, new_rows, new_qual, new_len, bank, bank_norms, bank_qual, bank_len,
+                    scales: Optional[torch.Tensor] = None, usage: Optional[torch.Tensor] = None,
+                    usage0: float = 0.0, stream=None):
+    """Rows ``at`` [n] of the bank become ``new_rows``, with their norms, labels and
+    usage; entries of ``at`` outside the bank (-1) are passed over."""
+    code, N, d = _bank(bank, bank_norms, scales, None)
+    M = _labels(bank_qual, bank_len, N)
+    if not isinstance(at, torch.Tensor) or at.dim() != 1:
+        raise ValueError("at: expected a 1-d tensor")
+    n = int(at.shape[0])
+    _expect(at, torch.int32, (n,), "at")
+    if not isinstance(new_rows, torch.Tensor) or new_rows.dim() != 2:
+        raise ValueError("new_rows: expected a 2-d tensor")
+    _expect(new_rows, new_rows.dtype if code == RB_Q4 else bank.dtype, (n, d), "new_rows")
+    src = _embedding_code(new_rows, "new_rows")
+    _expect(new_qual, torch.float32, (n, M), "new_qual")
+    _expect(new_len, torch.float32, (n, M), "new_len")
+    _expect_opt(usage, torch.float32, (N,), "usage")
+    dev = bank.device
+    _one_device(dev, at=at, new_rows=new_rows, new_qual=new_qual, new_len=new_len,
+                bank_norms=bank_norms, bank_qual=bank_qual, bank_len=bank_len, scales=scales,
+                usage=usage)
+    with _on(dev):
+        _check(_lib.rb_bank_replace(_ptr(at), n, _ptr(new_rows), src, _ptr(new_qual),
+                                    _ptr(new_len), M, _ptr(bank), _ptr(scales), _ptr(bank_norms),
+                                    code, N, d, _ptr(bank_qual), _ptr(bank_len), _ptr(usage),
+                                    float(usage0), _stream(stream)), "rb_bank_replace")

@@ -18,7 +18,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librouteb.so")
 SOURCES = ["api.hip", "knn.hip", "route.hip", "scan_rq.hip", "scan_rq12.hip", "scan_rq16.hip",
            "scan_rq24.hip", "scan_rq32.hip", "scan_gemm.hip", "scan_res_bf16.hip",
-           "scan_res_f32.hip", "select.hip"]
+           "scan_res_f32.hip", "select.hip", "attend.hip", "attend_grad.hip", "bank_rows.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

@@ -7,6 +7,7 @@
 #include <mutex>
 
 #include "../../include/routebalance.h"
+#include "attend.hpp"
 #include "kernels.hpp"
 
 namespace {
@@ -278,6 +279,50 @@ rb_status route_batch(const void *queries, const void *bank, const float *bank_n
     return hip_status(e);
 }
 
+// Sizes of a bank that may also be held in 4 bits.
+rb_status check_attend_dims(rb_dtype dt, int B, int N, int d)
+{
+    const rb_status s = check_embed_dims(dt == RB_Q4 ? RB_BF16 : dt, N, d);
+    if (s != RB_OK)
+        return s;
+    return B < 0 || (dt == RB_Q4 && d % 32 != 0) ? RB_ERR_DIMS : RB_OK;
+}
+
+bool beta_ok(float beta) { return beta >= 1e-30f && beta <= 1e30f; }   // (no NaN)
+
+rb_status check_ws(const void *ws, size_t have, size_t need)
+{
+    if (!ws || have < need)
+        return RB_ERR_WORKSPACE;
+    return aligned(ws, 256) ? RB_OK : RB_ERR_ALIGN;
+}
+
+rb::AttendBank attend_bank(const void *queries, const void *bank, const uint8_t *scales,
+                           const float *norms, const uint8_t *mask, int B, int N, int d, float beta)
+{
+    rb::AttendBank a;
+    a.queries = (const uint8_t *)queries;
+    a.rows = (const uint8_t *)bank;
+    a.scales = scales;
+    a.norms = norms;
+    a.mask = mask;
+    a.B = B;
+    a.N = N;
+    a.d = d;
+    a.c = (float)(2.0 * (double)beta * 1.4426950408889634);
+    return a;
+}
+
+// The plans' callers: sizes already checked.
+template <typename P, typename F>
+rb_status attend_plan(P *p, F make)
+{
+    int cu = 0;
+    if (num_cu(&cu) != 0)
+        return RB_ERR_HIP;
+    return make(cu, p) ? RB_OK : RB_ERR_DIMS;
+}
+
 }  // namespace
 
 extern "C" {
@@ -297,6 +342,7 @@ const char *rb_status_string(rb_status s)
     case RB_ERR_SCRATCH:
         return "RB_ERR_SCRATCH: these sizes need more workspace than the library's static "
                "RB_SCRATCH_BYTES";
+    case RB_ERR_VALUE: return "RB_ERR_VALUE: a scalar argument is out of range";
     }
     return "unknown rb_status";
 }
@@ -549,6 +595,280 @@ rb_status rb_profile_scan_events(void *begin, void *end)
 {
     rb::set_scan_events((hipEvent_t)begin, (hipEvent_t)end);
     return RB_OK;
+}
+
+rb_status rb_attend_workspace_size(int B, int N, int d, rb_dtype dtype, int M, size_t *bytes)
+{
+    if (!bytes)
+        return RB_ERR_NULL;
+    rb_status s = check_attend_dims(dtype, B, N, d);
+    if (s != RB_OK)
+        return s;
+    if (M < 1 || M > RB_MAX_M)
+        return RB_ERR_DIMS;
+    *bytes = 0;
+    if (B == 0)
+        return RB_OK;
+    rb::AttendPlan p;
+    s = attend_plan(&p, [&](int cu, rb::AttendPlan *q) {
+        return rb::plan_attend(B, N, d, (int)dtype, M, cu, q);
+    });
+    if (s == RB_OK)
+        *bytes = p.bytes;
+    return s;
+}
+
+rb_status rb_attend(const void *queries, const void *bank, const uint8_t *scales,
+                    const float *bank_norms, rb_dtype dtype, int B, int N, int d, float beta,
+                    const uint8_t *row_mask, const float *bank_qual, const float *bank_len, int M,
+                    float *q_hat, float *l_hat, float *lse, void *ws, size_t ws_bytes,
+                    void *stream)
+{
+    rb_status s = check_attend_dims(dtype, B, N, d);
+    if (s != RB_OK)
+        return s;
+    if (M < 1 || M > RB_MAX_M)
+        return RB_ERR_DIMS;
+    if (!beta_ok(beta))
+        return RB_ERR_VALUE;
+    if (B == 0)
+        return RB_OK;
+    if (!queries || !bank || !bank_norms || !bank_qual || !bank_len || !q_hat || !l_hat ||
+        (dtype == RB_Q4 && !scales))
+        return RB_ERR_NULL;
+    if (!aligned(queries, 16) || !aligned(bank, 16))
+        return RB_ERR_ALIGN;
+    rb::AttendPlan p;
+    s = attend_plan(&p, [&](int cu, rb::AttendPlan *q) {
+        return rb::plan_attend(B, N, d, (int)dtype, M, cu, q);
+    });
+    if (s != RB_OK || (s = check_ws(ws, ws_bytes, p.bytes)) != RB_OK)
+        return s;
+    return hip_status(rb::launch_attend(
+        p, attend_bank(queries, bank, scales, bank_norms, row_mask, B, N, d, beta), bank_qual,
+        bank_len, M, q_hat, l_hat, lse, ws, (hipStream_t)stream));
+}
+
+rb_status rb_attend_backward_workspace_size(int B, int N, int d, rb_dtype dtype, int M,
+                                            size_t *bytes)
+{
+    if (!bytes)
+        return RB_ERR_NULL;
+    rb_status s = check_embed_dims(dtype, N, d);
+    if (s != RB_OK)
+        return s;
+    if (B < 0 || M < 1 || M > RB_MAX_M)
+        return RB_ERR_DIMS;
+    *bytes = 0;
+    if (B == 0)
+        return RB_OK;
+    rb::GradPlan p;
+    s = attend_plan(&p, [&](int cu, rb::GradPlan *q) {
+        return rb::plan_grad(B, N, d, (int)dtype, M, cu, q);
+    });
+    if (s == RB_OK)
+        *bytes = p.bytes;
+    return s;
+}
+
+rb_status rb_attend_backward(const void *queries, const void *bank, const float *bank_norms,
+                             rb_dtype dtype, int B, int N, int d, float beta,
+                             const uint8_t *row_mask, const float *bank_qual,
+                             const float *bank_len, int M, const float *q_hat, const float *l_hat,
+                             const float *lse, const float *dq_hat, const float *dl_hat,
+                             const float *dlse, void *d_queries, void *d_bank, float *d_qual,
+                             float *d_len, float *d_beta, void *ws, size_t ws_bytes,
+                             void *stream)
+{
+    rb_status s = check_embed_dims(dtype, N, d);
+    if (s != RB_OK)
+        return s;
+    if (B < 0 || M < 1 || M > RB_MAX_M)
+        return RB_ERR_DIMS;
+    if (!beta_ok(beta))
+        return RB_ERR_VALUE;
+    if (!aligned(d_queries, 16) || !aligned(d_bank, 16))
+        return RB_ERR_ALIGN;
+    if (B == 0) {
+        const size_t row = (size_t)d * (dtype == RB_BF16 ? 2 : 4);
+        hipError_t e = hipSuccess;
+        if (d_bank)
+            e = rb::launch_zero(d_bank, (size_t)N * row, (hipStream_t)stream);
+        if (e == hipSuccess && d_qual)
+            e = rb::launch_zero(d_qual, (size_t)N * M * 4, (hipStream_t)stream);
+        if (e == hipSuccess && d_len)
+            e = rb::launch_zero(d_len, (size_t)N * M * 4, (hipStream_t)stream);
+        return hip_status(e);
+    }
+    if (!queries || !bank || !bank_norms || !bank_qual || !bank_len || !q_hat || !l_hat || !lse ||
+        !dq_hat || !dl_hat)
+        return RB_ERR_NULL;
+    if (!aligned(queries, 16) || !aligned(bank, 16))
+        return RB_ERR_ALIGN;
+    rb::GradPlan p;
+    s = attend_plan(&p, [&](int cu, rb::GradPlan *q) {
+        return rb::plan_grad(B, N, d, (int)dtype, M, cu, q);
+    });
+    if (s != RB_OK || (s = check_ws(ws, ws_bytes, p.bytes)) != RB_OK)
+        return s;
+    if (!d_queries && !d_bank && !d_qual && !d_len && !d_beta)
+        return RB_OK;
+    rb::GradArgs g;
+    g.qual = bank_qual;
+    g.len = bank_len;
+    g.M = M;
+    g.q_hat = q_hat;
+    g.l_hat = l_hat;
+    g.lse = lse;
+    g.dq_hat = dq_hat;
+    g.dl_hat = dl_hat;
+    g.dlse = dlse;
+    g.d_queries = d_queries;
+    g.d_bank = d_bank;
+    g.d_qual = d_qual;
+    g.d_len = d_len;
+    g.d_beta = d_beta;
+    g.beta = beta;
+    return hip_status(rb::launch_grad(
+        p, attend_bank(queries, bank, nullptr, bank_norms, row_mask, B, N, d, beta), g, ws,
+        (hipStream_t)stream));
+}
+
+rb_status rb_attend_usage_workspace_size(int B, int N, int d, rb_dtype dtype, size_t *bytes)
+{
+    if (!bytes)
+        return RB_ERR_NULL;
+    rb_status s = check_attend_dims(dtype, B, N, d);
+    if (s != RB_OK)
+        return s;
+    *bytes = 0;
+    if (B == 0)
+        return RB_OK;
+    rb::UsagePlan p;
+    s = attend_plan(&p, [&](int cu, rb::UsagePlan *q) {
+        return rb::plan_usage(B, N, d, (int)dtype, cu, q);
+    });
+    if (s == RB_OK)
+        *bytes = p.bytes;
+    return s;
+}
+
+rb_status rb_attend_usage(const void *queries, const void *bank, const uint8_t *scales,
+                          const float *bank_norms, rb_dtype dtype, int B, int N, int d, float beta,
+                          const uint8_t *row_mask, const float *lse, float decay, float *usage,
+                          void *ws, size_t ws_bytes, void *stream)
+{
+    rb_status s = check_attend_dims(dtype, B, N, d);
+    if (s != RB_OK)
+        return s;
+    if (!beta_ok(beta) || !(decay >= 0.f && decay <= 1.f))
+        return RB_ERR_VALUE;
+    if (!usage)
+        return RB_ERR_NULL;
+    if (B == 0)
+        return hip_status(rb::launch_decay(usage, N, decay, (hipStream_t)stream));
+    if (!queries || !bank || !bank_norms || !lse || (dtype == RB_Q4 && !scales))
+        return RB_ERR_NULL;
+    if (!aligned(queries, 16) || !aligned(bank, 16))
+        return RB_ERR_ALIGN;
+    rb::UsagePlan p;
+    s = attend_plan(&p, [&](int cu, rb::UsagePlan *q) {
+        return rb::plan_usage(B, N, d, (int)dtype, cu, q);
+    });
+    if (s != RB_OK || (s = check_ws(ws, ws_bytes, p.bytes)) != RB_OK)
+        return s;
+    return hip_status(rb::launch_usage(
+        p, attend_bank(queries, bank, scales, bank_norms, row_mask, B, N, d, beta), lse, decay,
+        usage, ws, (hipStream_t)stream));
+}
+
+rb_status rb_bank_pack(const void *bank, rb_dtype dtype, int N, int d, uint8_t *rows,
+                       uint8_t *scales, float *norms, void *stream)
+{
+    const rb_status s = check_embed_dims(dtype, N, d);
+    if (s != RB_OK)
+        return s;
+    if (d % 32 != 0)
+        return RB_ERR_DIMS;
+    if (!bank || !rows || !scales || !norms)
+        return RB_ERR_NULL;
+    if (!aligned(bank, 16) || !aligned(rows, 16))
+        return RB_ERR_ALIGN;
+    rb::RowsArgs a{};
+    a.src = (const uint8_t *)bank;
+    a.n = a.N = N;
+    a.d = d;
+    a.rows = rows;
+    a.scales = scales;
+    a.norms = norms;
+    return hip_status(rb::launch_write_rows((int)dtype, rb::AT_Q4, a, (hipStream_t)stream));
+}
+
+rb_status rb_evict_workspace_size(int N, size_t *bytes)
+{
+    if (!bytes)
+        return RB_ERR_NULL;
+    if (N < 1)
+        return RB_ERR_DIMS;
+    *bytes = rb::evict_bytes(N);
+    return RB_OK;
+}
+
+rb_status rb_bank_evict(const float *usage, const uint8_t *may_go, int N, int n, int32_t *victims,
+                        void *ws, size_t ws_bytes, void *stream)
+{
+    if (N < 1 || n < 0 || n > N)
+        return RB_ERR_DIMS;
+    if (n == 0)
+        return RB_OK;
+    if (!usage || !victims)
+        return RB_ERR_NULL;
+    const rb_status s = check_ws(ws, ws_bytes, rb::evict_bytes(N));
+    if (s != RB_OK)
+        return s;
+    return hip_status(
+        rb::launch_evict(usage, may_go, N, n, victims, ws, (hipStream_t)stream));
+}
+
+rb_status rb_bank_replace(const int32_t *at, int n, const void *new_rows, rb_dtype src_dtype,
+                          const float *new_qual, const float *new_len, int M, void *bank,
+                          uint8_t *scales, float *bank_norms, rb_dtype dtype, int N, int d,
+                          float *bank_qual, float *bank_len, float *usage, float usage0,
+                          void *stream)
+{
+    rb_status s = check_attend_dims(dtype, n, N, d);
+    if (s != RB_OK)
+        return s;
+    if ((src_dtype != RB_F32 && src_dtype != RB_BF16) || (dtype != RB_Q4 && src_dtype != dtype))
+        return RB_ERR_DTYPE;
+    if (M < 1 || M > RB_MAX_M)
+        return RB_ERR_DIMS;
+    if (!isfinite(usage0))
+        return RB_ERR_VALUE;
+    if (n == 0)
+        return RB_OK;
+    if (!at || !new_rows || !new_qual || !new_len || !bank || !bank_norms || !bank_qual ||
+        !bank_len || (dtype == RB_Q4 && !scales))
+        return RB_ERR_NULL;
+    if (!aligned(new_rows, 16) || !aligned(bank, 16))
+        return RB_ERR_ALIGN;
+    rb::RowsArgs a{};
+    a.src = (const uint8_t *)new_rows;
+    a.at = at;
+    a.n = n;
+    a.N = N;
+    a.d = d;
+    a.M = M;
+    a.rows = (uint8_t *)bank;
+    a.scales = scales;
+    a.norms = bank_norms;
+    a.new_qual = new_qual;
+    a.new_len = new_len;
+    a.qual = bank_qual;
+    a.len = bank_len;
+    a.usage = usage;
+    a.usage0 = usage0;
+    return hip_status(rb::launch_write_rows((int)src_dtype, (int)dtype, a, (hipStream_t)stream));
 }
 
 rb_status rb_advance_state(const rb_instances *inst, int I, float dt_seconds, void *stream)

@@ -1,0 +1,379 @@
+// Attention of requests over the labelled bank: the forward pass.
+#include "attend_scan.hpp"
+
+#include <math.h>
+
+namespace rb {
+
+namespace {
+
+constexpr int AT_RING = 6;       // k-steps of bank rows in flight
+// A running maximum is raised when a score passes it by this many powers of
+// two: weights stay below 2^16 and few slabs rescale what went before.
+constexpr float AT_SLACK = 16.f;
+
+struct AttendArgs {
+    AttendBank b;
+    const float *qual, *len;
+    int M, nks, n_chunks, n_qt;
+    long slabs;
+    float *ml;   // [n_chunks][B][2] maximum (in powers of two) and sum of the weights
+    float *o;    // [n_chunks][n_lt][B][ct * 16] sums of weighted labels
+};
+
+// One workgroup per (share of the bank, tile of NG * 16 requests, tile of CT *
+// 16 label columns); each wave has its own part of the share, its own running
+// maximum and sums, and the waves' are joined in LDS at the end.
+//   scores   a = <q, x> - |q|^2/2 - |x|^2/2 (MFMA), t = c*a
+//   maximum  raised now and then, the sums rescaled when it is
+//   weights  p = 2^(t - maximum), their sum, and sum of p * label as a second
+//            MFMA (fp32, 16 label columns x 16 requests, 4 rows): its operand
+//            p[row 4*(lane/16) + e][request lane%16] is register e of the
+//            scores as it stands.
+template <int DT, int NG, int CT>
+__global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const AttendArgs A)
+{
+    extern __shared__ __align__(16) uint8_t smem[];
+    i32x4 *qs = (i32x4 *)smem;
+    int t, ch;
+    chunk_and_tile(A.n_chunks, A.n_qt, &ch, &t);
+    if (ch >= A.n_chunks)
+        return;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int n_waves = blockDim.x >> 6;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 15, jg = lane >> 4;
+    const int q0 = t * NG * 16, lt = blockIdx.y;
+    const long gw = (long)ch * n_waves + wave, n_gw = (long)A.n_chunks * n_waves;
+    const long s0 = gw * A.slabs / n_gw, s1 = (gw + 1) * A.slabs / n_gw;
+    const int N = A.b.N;
+    const float c = A.b.c;
+
+    load_requests<DT, NG>(A.b, A.nks, q0, qs, wave, n_waves, lane);
+    wait_vmcnt<0>();
+    stream_barrier();
+
+    // -|q|^2/2 of this lane's requests, from the fragments in LDS
+    float hq[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        float sum = 0.f;
+        for (int f = 0; f < A.nks * AtElem<DT>::SUB; ++f)
+            sum = sumsq16<DT == AT_F32 ? 0 : 1>(qs[(f * NG + g) * WAVE + lane], sum);
+        hq[g] = -0.5f * rows_reduce(sum, [](float x, float y) { return x + y; });
+    }
+
+    // this lane's label columns
+    const float *lab[CT];
+    bool lab_ok[CT];
+#pragma unroll
+    for (int k = 0; k < CT; ++k) {
+        const int cc = (lt * CT + k) * 16 + col;
+        lab_ok[k] = cc < 2 * A.M;
+        lab[k] = cc < A.M ? A.qual + cc : lab_ok[k] ? A.len + (cc - A.M) : A.qual;
+    }
+    float ref[NG], sub[NG], l[NG];
+    f32x4 o[NG][CT];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        ref[g] = -INFINITY;   // the maximum that the sums are relative to
+        sub[g] = 0.f;         // the same, 0 where there is none yet
+        l[g] = 0.f;
+#pragma unroll
+        for (int k = 0; k < CT; ++k)
+            o[g][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    // norms, mask and labels of a slab: this lane's rows 16*r + 4*jg + e
+    f32x4 nh[AT_RT];             // -|x|^2/2, -inf for rows masked or past the bank
+    float v[AT_RT][4][CT];
+    auto side = [&](long slab) {
+        const long r0 = slab * AT_SLAB + jg * 4;
+#pragma unroll
+        for (int r = 0; r < AT_RT; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const long row = r0 + r * 16 + e;
+                const bool in = row < N;
+                const size_t at = in ? (size_t)row : 0;
+                const bool ok = in && (!A.b.mask || A.b.mask[at] != 0);
+                nh[r][e] = ok ? -0.5f * A.b.norms[at] : -INFINITY;
+#pragma unroll
+                for (int k = 0; k < CT; ++k) {
+                    const float x = lab[k][at * A.M];
+                    v[r][e][k] = ok && lab_ok[k] ? x : 0.f;
+                }
+            }
+    };
+    auto start = [&](int slab, f32x4(&acc)[AT_RT][NG]) {
+        side(min(s0 + slab, A.slabs - 1));
+#pragma unroll
+        for (int r = 0; r < AT_RT; ++r)
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    acc[r][g][e] = nh[r][e] + hq[g];
+    };
+    auto end = [&](int, f32x4(&acc)[AT_RT][NG]) {
+        bool raise = false;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            float m = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < AT_RT; ++r)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    // (a masked row may hold anything)
+                    if (A.b.mask)
+                        acc[r][g][e] = nh[r][e] == -INFINITY ? -INFINITY : acc[r][g][e];
+                    m = fmaxf(m, acc[r][g][e]);
+                }
+            raise |= c * m > ref[g] + AT_SLACK;
+        }
+        if (ballot(raise)) {
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                float m = -INFINITY;
+#pragma unroll
+                for (int r = 0; r < AT_RT; ++r)
+                    m = fmaxf(m, max4(acc[r][g]));
+                m = rows_reduce(c * m, [](float x, float y) { return fmaxf(x, y); });
+                const float up = fmaxf(ref[g], m);
+                const float f = ref[g] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[g] - up);
+                ref[g] = up;
+                sub[g] = up == -INFINITY ? 0.f : up;
+                l[g] *= f;
+#pragma unroll
+                for (int k = 0; k < CT; ++k)
+                    o[g][k] *= f;
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < AT_RT; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    const float p =
+                        __builtin_amdgcn_exp2f(fmaf(c, acc[r][g][e], -sub[g]));
+                    l[g] += p;
+#pragma unroll
+                    for (int k = 0; k < CT; ++k)
+                        o[g][k] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[r][e][k], p, o[g][k], 0,
+                                                                      0, 0);
+                }
+    };
+    scan_slabs<DT, NG, AT_RING, false>(A.b, A.nks, qs, s0, s1, lane, start, end);
+
+    // ---- the waves' sums, joined (the request tile's LDS is free now)
+    constexpr int W = 2 + 16 * CT;
+    float *jn = (float *)smem;   // [n_waves][NG * 16][W]
+    stream_barrier();
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        const float ls = rows_reduce(l[g], [](float x, float y) { return x + y; });
+        float *at = jn + (wave * NG * 16 + g * 16 + col) * W;
+        if (jg == 0) {
+            at[0] = ref[g];
+            at[1] = ls;
+        }
+#pragma unroll
+        for (int k = 0; k < CT; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                at[2 + k * 16 + jg * 4 + e] = o[g][k][e];
+    }
+    stream_barrier();
+    for (int i = tid; i < NG * 16 * (W - 1); i += blockDim.x) {
+        const int q = i / (W - 1), x = i - q * (W - 1);   // x 0: the sum, else a column
+        if (q0 + q >= A.b.B)
+            continue;
+        float m = -INFINITY, sum = 0.f;
+        for (int w = 0; w < n_waves; ++w)
+            m = fmaxf(m, jn[(w * NG * 16 + q) * W]);
+        for (int w = 0; w < n_waves; ++w) {
+            const float *at = jn + (w * NG * 16 + q) * W;
+            if (at[0] != -INFINITY)
+                sum = fmaf(__builtin_amdgcn_exp2f(at[0] - m), at[1 + x], sum);
+        }
+        if (x > 0) {
+            A.o[(((size_t)ch * gridDim.y + lt) * A.b.B + q0 + q) * (16 * CT) + x - 1] = sum;
+        } else if (lt == 0) {
+            float *ml = A.ml + ((size_t)ch * A.b.B + q0 + q) * 2;
+            ml[0] = m;
+            ml[1] = sum;
+        }
+    }
+}
+
+// The shares' sums joined: one workgroup of 256 threads per request.
+__global__ __launch_bounds__(256) void attend_join_kernel(const float *ml, const float *o,
+                                                          int n_chunks, int n_lt, int width, int B,
+                                                          int M, float *q_hat, float *l_hat,
+                                                          float *lse)
+{
+    __shared__ float red[256], wts[256];
+    const int b = blockIdx.x, tid = threadIdx.x;
+    float m = -INFINITY;
+    for (int ch = tid; ch < n_chunks; ch += 256)
+        m = fmaxf(m, ml[((size_t)ch * B + b) * 2]);
+    red[tid] = m;
+    __syncthreads();
+    for (int k = 128; k > 0; k >>= 1) {
+        if (tid < k)
+            red[tid] = fmaxf(red[tid], red[tid + k]);
+        __syncthreads();
+    }
+    m = red[0];
+    __syncthreads();
+    float sum = 0.f;
+    for (int ch = tid; ch < n_chunks; ch += 256) {
+        const float *at = ml + ((size_t)ch * B + b) * 2;
+        if (at[0] != -INFINITY)
+            sum = fmaf(__builtin_amdgcn_exp2f(at[0] - m), at[1], sum);
+    }
+    red[tid] = sum;
+    __syncthreads();
+    for (int k = 128; k > 0; k >>= 1) {
+        if (tid < k)
+            red[tid] += red[tid + k];
+        __syncthreads();
+    }
+    const float total = red[0];
+    if (tid == 0 && lse)
+        lse[b] = (m + __builtin_amdgcn_logf(total)) * LN2;
+    // columns: 16 of them at a time, 16 shares side by side
+    const int col = tid & 15, part = tid >> 4;
+    for (int c0 = 0; c0 < 2 * M; c0 += 16) {
+        const int cc = c0 + col, tile = cc / width;
+        float s = 0.f;
+        for (int k0 = 0; k0 < n_chunks; k0 += 256) {
+            __syncthreads();
+            const int ch = k0 + tid;
+            const float x = ch < n_chunks ? ml[((size_t)ch * B + b) * 2] : -INFINITY;
+            wts[tid] = x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - m);
+            __syncthreads();
+            if (cc < 2 * M)
+                for (int k = part; k < min(256, n_chunks - k0); k += 16)
+                    if (wts[k] != 0.f)
+                        s = fmaf(wts[k],
+                                 o[(((size_t)(k0 + k) * n_lt + tile) * B + b) * width + cc -
+                                   tile * width],
+                                 s);
+        }
+        __syncthreads();
+        red[tid] = s;
+        __syncthreads();
+        if (tid < 16 && cc < 2 * M) {
+            s = 0.f;
+            for (int k = 0; k < 16; ++k)
+                s += red[k * 16 + col];
+            s /= total;
+            if (cc < M)
+                q_hat[(size_t)b * M + cc] = s;
+            else
+                l_hat[(size_t)b * M + cc - M] = s;
+        }
+    }
+}
+
+template <int DT, int NG, int CT>
+hipError_t launch_one(const AttendPlan &p, const AttendArgs &a, hipStream_t s)
+{
+    auto kern = attend_kernel<DT, NG, CT>;
+    const hipError_t e = hipFuncSetAttribute(
+        (const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.lds_bytes);
+    if (e != hipSuccess)
+        return e;
+    hipLaunchKernelGGL(kern, dim3(p.n_chunks * p.n_qt, p.n_lt), dim3(p.waves * WAVE), p.lds_bytes,
+                       s, a);
+    return hipGetLastError();
+}
+
+template <int DT, int CT>
+hipError_t launch_ng(const AttendPlan &p, const AttendArgs &a, hipStream_t s)
+{
+    switch (p.ng) {
+    case 1: return launch_one<DT, 1, CT>(p, a, s);
+    case 2: return launch_one<DT, 2, CT>(p, a, s);
+    case 4: return launch_one<DT, 4, CT>(p, a, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+template <int DT>
+hipError_t launch_dt(const AttendPlan &p, const AttendArgs &a, hipStream_t s)
+{
+    return p.ct == 1 ? launch_ng<DT, 1>(p, a, s) : launch_ng<DT, 2>(p, a, s);
+}
+
+size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+}  // namespace
+
+bool plan_attend(int B, int N, int d, int dtype, int M, int n_cu, AttendPlan *p)
+{
+    const int ks = at_ks(dtype);
+    p->dtype = dtype;
+    p->nks = (d + ks - 1) / ks;
+    p->slabs = (int)(((long)N + AT_SLAB - 1) / AT_SLAB);
+    p->ct = 2 * M <= 16 ? 1 : 2;
+    p->n_lt = (2 * M + 16 * p->ct - 1) / (16 * p->ct);
+    const size_t group = (size_t)p->nks * ks * (dtype == AT_F32 ? 4 : 2) * 16;
+    int ng = B <= 16 ? 1 : B <= 32 ? 2 : 4;
+    while (ng > 1 && group * ng > (size_t)AT_LDS)
+        ng /= 2;
+    if (group * ng > (size_t)AT_LDS)
+        return false;
+    p->ng = ng;
+    p->n_qt = (B + ng * 16 - 1) / (ng * 16);
+    // one workgroup per compute unit, as far as there are slabs for its waves;
+    // a wave's part of the bank stays under 1 GB (32-bit offsets)
+    const long tiles = (long)p->n_qt * p->n_lt;
+    long chunks = n_cu / tiles;
+    const long by_size =
+        ((long)p->slabs * AT_SLAB * at_row_bytes(dtype, d) >> 30) / AT_WAVES + 1;
+    if (chunks < by_size)
+        chunks = by_size;
+    if (chunks > p->slabs)
+        chunks = p->slabs;
+    if (chunks < 1)
+        chunks = 1;
+    p->n_chunks = (int)chunks;
+    const long per = (p->slabs + chunks - 1) / chunks;
+    p->waves = per < AT_WAVES ? (int)per : AT_WAVES;
+    const size_t join = (size_t)p->waves * ng * 16 * (2 + 16 * p->ct) * 4;
+    p->lds_bytes = group * ng > join ? group * ng : join;
+    p->off_ml = 0;
+    p->off_o = up256((size_t)chunks * B * 2 * 4);
+    p->bytes = p->off_o + up256((size_t)chunks * p->n_lt * B * 16 * p->ct * 4);
+    return true;
+}
+
+hipError_t launch_attend(const AttendPlan &p, const AttendBank &b, const float *qual,
+                         const float *len, int M, float *q_hat, float *l_hat, float *lse, void *ws,
+                         hipStream_t s)
+{
+    AttendArgs a;
+    a.b = b;
+    a.qual = qual;
+    a.len = len;
+    a.M = M;
+    a.nks = p.nks;
+    a.n_chunks = p.n_chunks;
+    a.n_qt = p.n_qt;
+    a.slabs = p.slabs;
+    a.ml = (float *)((uint8_t *)ws + p.off_ml);
+    a.o = (float *)((uint8_t *)ws + p.off_o);
+    const hipError_t e = p.dtype == AT_F32    ? launch_dt<AT_F32>(p, a, s)
+                         : p.dtype == AT_BF16 ? launch_dt<AT_BF16>(p, a, s)
+                                              : launch_dt<AT_Q4>(p, a, s);
+    if (e != hipSuccess)
+        return e;
+    hipLaunchKernelGGL(attend_join_kernel, dim3(b.B), dim3(256), 0, s, a.ml, a.o, p.n_chunks,
+                       p.n_lt, 16 * p.ct, b.B, M, q_hat, l_hat, lse);
+    return hipGetLastError();
+}
+
+}  // namespace rb

@@ -1,0 +1,116 @@
+// Attention of requests over the labelled bank: argument blocks, host plan and
+// launchers (attend.hip the forward pass, attend_grad.hip the passes that
+// recompute its probabilities, bank_rows.hip the rows of the bank themselves).
+//
+// Request b weighs bank row n by p[b][n] = exp(-beta*|q_b - x_n|^2) / Z_b, Z_b
+// the sum over the rows whose mask is not 0. All kernels work with
+//   a[b][n] = <q, x> - |q|^2/2 - |x|^2/2 = -|q - x|^2/2,
+// the accumulators of a matrix product that starts from the norms, and with
+// powers of two: p = 2^(c*a - lse*log2(e)), c = 2*beta*log2(e).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace rb {
+
+constexpr int AT_F32 = 0, AT_BF16 = 1, AT_Q4 = 2;   // rb_dtype of a bank
+constexpr int AT_WAVES = 8;                         // most waves of a workgroup
+constexpr int AT_LDS = 160 * 1024;                  // bytes of LDS of a compute unit
+
+struct AttendBank {
+    const uint8_t *queries, *rows, *scales;   // scales: 4-bit banks only
+    const float *norms;
+    const uint8_t *mask;                      // [N] or null
+    int B, N, d;
+    float c;                                  // 2 * beta * log2(e)
+};
+
+struct AttendPlan {
+    int dtype, ng;         // request tile: ng groups of 16
+    int n_qt, n_chunks;    // request tiles, shares of the bank
+    int waves, nks;        // waves of a workgroup, k-steps of a row
+    int n_lt;              // tiles of label columns
+    int ct;                //   of ct * 16 columns each
+    int slabs;             // pieces of 32 rows
+    size_t lds_bytes;
+    size_t off_ml, off_o, bytes;   // workspace: partial maxima and sums, partial averages
+};
+
+// The forward pass on a device of n_cu compute units; false if no layout fits.
+bool plan_attend(int B, int N, int d, int dtype, int M, int n_cu, AttendPlan *p);
+
+hipError_t launch_attend(const AttendPlan &p, const AttendBank &a, const float *qual,
+                         const float *len, int M, float *q_hat, float *l_hat, float *lse, void *ws,
+                         hipStream_t s);
+
+// The accumulated weight of the bank's rows: usage = decay * usage + sum over
+// the batch of p.
+struct UsagePlan {
+    int dtype, ng, n_qt, n_chunks, waves, nks, slabs;
+    size_t lds_bytes;
+    size_t off_side, off_part, bytes;   // per request; partial sums per request tile
+};
+
+bool plan_usage(int B, int N, int d, int dtype, int n_cu, UsagePlan *p);
+
+hipError_t launch_usage(const UsagePlan &p, const AttendBank &a, const float *lse, float decay,
+                        float *usage, void *ws, hipStream_t s);
+
+// usage *= decay, and zeros, for batches of no requests.
+hipError_t launch_decay(float *usage, int N, float decay, hipStream_t s);
+hipError_t launch_zero(void *p, size_t bytes, hipStream_t s);   // bytes a multiple of 4
+
+// The gradients. The bank goes by in parts, each in three passes: the scores'
+// gradient ds (and what needs no further product), then d_queries += ds * rows,
+// then d_bank = ds^T * queries.
+struct GradPlan {
+    int dtype, ng, n_qt, n_chunks, waves, nks, slabs;
+    bool tab;             // the label gradients of a request tile fit LDS
+    int n_blk;            // blocks of requests of one fragment of ds (32, fp32 16)
+    int pitch;            // floats of a request's label gradients
+    int part_slabs;       // slabs of a part
+    int q_chunks;         // shares of a part in the d_queries pass
+    size_t lds_bytes;
+    size_t off_side, off_dout, off_qpack, off_ds, off_rowsum, off_lab, off_req, off_dq, bytes;
+};
+
+struct GradArgs {
+    const float *qual, *len;
+    int M;
+    const float *q_hat, *l_hat, *lse, *dq_hat, *dl_hat, *dlse;   // dlse may be null
+    void *d_queries, *d_bank;                                    // may be null
+    float *d_qual, *d_len, *d_beta;                              // may be null
+    float beta;
+};
+
+bool plan_grad(int B, int N, int d, int dtype, int M, int n_cu, GradPlan *p);
+
+hipError_t launch_grad(const GradPlan &p, const AttendBank &a, const GradArgs &g, void *ws,
+                       hipStream_t s);
+
+// Rows of the bank (bank_rows.hip). Row j of src (fp32 or bf16) becomes row
+// at[j] (j, if at is null) of the bank, with its norm; rows outside [0, N) are
+// left out. Labels and usage where their pointers are not null.
+struct RowsArgs {
+    const uint8_t *src;
+    const int32_t *at;
+    int n, N, d, M;
+    uint8_t *rows, *scales;
+    float *norms;
+    const float *new_qual, *new_len;
+    float *qual, *len, *usage;
+    float usage0;
+};
+
+hipError_t launch_write_rows(int src_dtype, int dtype, const RowsArgs &a, hipStream_t s);
+
+// The n rows of least usage (equal usage: the lower row first) of those whose
+// may_go is not 0, ascending; -1 behind them where there are fewer.
+size_t evict_bytes(int N);
+
+hipError_t launch_evict(const float *usage, const uint8_t *may_go, int N, int n, int32_t *victims,
+                        void *ws, hipStream_t s);
+
+}  // namespace rb

@@ -1,0 +1,165 @@
+// The pass over the bank that the attention kernels share (gfx950, wave64).
+#pragma once
+
+#include "attend.hpp"
+#include "knn_common.hpp"
+
+namespace rb {
+
+namespace {
+
+constexpr int AT_RT = 2;                 // 16-row tiles of a slab
+constexpr int AT_SLAB = 16 * AT_RT;      // bank rows a wave takes at a time
+constexpr float LN2 = 0.693147180559945309f, LOG2E = 1.442695040888963407f;
+
+// What 16 bytes of a bank row per lane are (a k-step: 64 bytes of each of 16
+// rows), and how many request fragments of 16 bytes per lane meet them.
+template <int DT> struct AtElem;
+template <> struct AtElem<AT_F32> { static constexpr int KS = 16, SUB = 1, QSZ = 4; };
+template <> struct AtElem<AT_BF16> { static constexpr int KS = 32, SUB = 1, QSZ = 2; };
+template <> struct AtElem<AT_Q4> { static constexpr int KS = 128, SUB = 4, QSZ = 2; };
+
+inline __host__ __device__ int at_ks(int dtype)
+{
+    return dtype == AT_F32 ? 16 : dtype == AT_BF16 ? 32 : 128;
+}
+inline __host__ __device__ uint32_t at_row_bytes(int dtype, int d)
+{
+    return (uint32_t)(dtype == AT_F32 ? d * 4 : dtype == AT_BF16 ? d * 2 : d / 2);
+}
+inline __host__ __device__ uint32_t at_query_bytes(int dtype, int d)
+{
+    return (uint32_t)(dtype == AT_F32 ? d * 4 : d * 2);
+}
+
+// The request tile (NG groups of 16 from request q0 on, every k-step) into LDS:
+// qs[(k-step * SUB + sub) * NG + group][lane], lane (request lane % 16, K part
+// lane / 16). Zero past the batch and past the row.
+template <int DT, int NG>
+__device__ __forceinline__ void load_requests(const AttendBank &A, int nks, int q0, i32x4 *qs,
+                                              int wave, int n_waves, int lane)
+{
+    using E = AtElem<DT>;
+    const uint32_t rowb = at_query_bytes(DT, A.d);
+    const int col = lane & 15, jg = lane >> 4;
+    // (a resource of this tile alone: a batch may pass 4 GB)
+    const int nq = min(A.B - q0, NG * 16);
+    const __amdgpu_buffer_rsrc_t rq =
+        make_rsrc(A.queries + (size_t)q0 * rowb, (uint32_t)nq * rowb);
+    for (int f = wave; f < nks * E::SUB * NG; f += n_waves) {
+        const int ks = f / (E::SUB * NG), rest = f - ks * E::SUB * NG;
+        const int sub = rest / NG, q = (rest - sub * NG) * 16 + col;
+        // the lane's first element: bank elements of the same lane and place
+        const int el = ks * E::KS + jg * (E::KS / 4) + sub * 8;
+        dma16(rq, qs + f * WAVE,
+              q < nq && el < A.d ? (uint32_t)q * rowb + (uint32_t)el * E::QSZ : OFF_NONE);
+    }
+}
+
+// A lane's 32 elements of 4 bits (codes of 0, 0.5, 1, 1.5, 2, 3, 4, 6, bit 3
+// the sign) times their scale, as four bf16 fragments: exact, every product is
+// a bf16 value.
+__device__ __forceinline__ i32x4 widen4(uint32_t codes, float scale)
+{
+    i32x4 r;
+    r[0] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
+    r[1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
+    r[2] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
+    r[3] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+    return r;
+}
+
+// One wave's pass over slabs [s0, s1) of the bank against the request tile in
+// LDS. Bank rows come from HBM straight into MFMA operand registers, R k-steps
+// ahead across slab ends, and no wave waits for another. start(slab, acc) sets
+// a slab's accumulators before its first product, end(slab, acc) takes them.
+// BANK_COLS false: acc[r][g][e] is of row 16*r + 4*(lane/16) + e and request
+// 16*g + lane%16; true: of row 16*r + lane%16 and request 16*g + 4*(lane/16) + e.
+template <int DT, int NG, int R, bool BANK_COLS, typename Start, typename End>
+__device__ __forceinline__ void scan_slabs(const AttendBank &A, int nks, const i32x4 *qs, long s0,
+                                           long s1, int lane, Start &&start, End &&end)
+{
+    using E = AtElem<DT>;
+    constexpr int MDT = DT == AT_F32 ? 0 : 1;
+    const int col = lane & 15, jg = lane >> 4;
+    const uint32_t rowb = at_row_bytes(DT, A.d);
+    const int n_slabs = (int)(s1 - s0);
+    const long row0 = s0 * AT_SLAB;
+    const int nrows = n_slabs > 0 ? (int)min((long)n_slabs * AT_SLAB, A.N - row0) : 0;
+    const __amdgpu_buffer_rsrc_t rbk =
+        make_rsrc(A.rows + (size_t)(nrows ? row0 : 0) * rowb, (uint32_t)nrows * rowb);
+    const int nsc = A.d / 32;   // scales of a row
+    const __amdgpu_buffer_rsrc_t rsc =
+        DT == AT_Q4 ? make_rsrc(A.scales + (size_t)(nrows ? row0 : 0) * nsc, (uint32_t)nrows * nsc)
+                    : rbk;
+    const bool tail_ok = (nks - 1) * E::KS + jg * (E::KS / 4) < A.d;
+    i32x4 ring[R][AT_RT];
+    uint8_t rsca[DT == AT_Q4 ? R : 1][AT_RT];
+    uint32_t lvo = (uint32_t)col * rowb + jg * 16;
+    uint32_t lsc = (uint32_t)col * nsc + jg;
+    int ls = 0;
+    auto issue = [&](auto U) {
+        constexpr int u = decltype(U)::value;
+        const bool none = ls == nks - 1 && !tail_ok;
+#pragma unroll
+        for (int r = 0; r < AT_RT; ++r) {
+            ring[u][r] = buffer_load16(rbk, none ? OFF_NONE : lvo + (uint32_t)r * 16 * rowb);
+            if constexpr (DT == AT_Q4)
+                rsca[u][r] = __builtin_amdgcn_raw_buffer_load_b8(
+                    rsc, (int)(none ? OFF_NONE : lsc + (uint32_t)(r * 16 * nsc)), 0, 0);
+        }
+        lvo += KSTEP_BYTES;
+        lsc += 4;
+        if (++ls == nks) {
+            ls = 0;
+            lvo += AT_SLAB * rowb - (uint32_t)nks * KSTEP_BYTES;
+            lsc += AT_SLAB * nsc - nks * 4;
+        }
+    };
+    static_for<0, R>([&](auto U) { issue(U); });
+
+    f32x4 acc[AT_RT][NG];
+    int slab = 0, s = 0;
+    if (n_slabs > 0)
+        start(0, acc);
+    const long n_pos = (long)n_slabs * nks;
+    for (long x = 0; x < n_pos; x += R) {
+        static_for<0, R>([&](auto U) {
+            constexpr int u = decltype(U)::value;
+            static_for<0, E::SUB>([&](auto T) {
+                constexpr int t = decltype(T)::value;
+                const i32x4 *fr = qs + (s * E::SUB + t) * NG * WAVE + lane;
+                i32x4 a[AT_RT];
+#pragma unroll
+                for (int r = 0; r < AT_RT; ++r) {
+                    if constexpr (DT == AT_Q4)
+                        a[r] = widen4((uint32_t)ring[u][r][t],
+                                      __uint_as_float((uint32_t)rsca[u][r] << 23));
+                    else
+                        a[r] = ring[u][r];
+                }
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    const i32x4 b = fr[g * WAVE];
+#pragma unroll
+                    for (int r = 0; r < AT_RT; ++r)
+                        acc[r][g] = BANK_COLS ? mfma_step<MDT>(b, a[r], acc[r][g])
+                                              : mfma_step<MDT>(a[r], b, acc[r][g]);
+                }
+            });
+            issue(U);
+            if (++s == nks) {
+                s = 0;
+                if (slab < n_slabs) {   // (past the share: nothing to take)
+                    end(slab, acc);
+                    ++slab;
+                    start(slab, acc);
+                }
+            }
+        });
+    }
+}
+
+}  // namespace
+
+}  // namespace rb

@@ -1,0 +1,369 @@
+"""Attention over the bank against 64 bits (GPU): forward, gradients, usage, in
+every type of bank, at the sizes and masks where the tiles end."""
+import math
+
+import pytest
+import torch
+
+import attend_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+
+
+def make(dtype, B, N, d, M, seed=0, mask=None, scale=1.0):
+    """Seeded inputs; mask: None, "some" (masked rows hold no numbers) or "all"."""
+    import paper_2606_17949_amd as rb
+    g = torch.Generator(device=DEV).manual_seed(1000 + seed)
+    centres = torch.randn(max(2, N // 40), d, generator=g, device=DEV)
+
+    def rows(n):
+        u = torch.randint(0, centres.shape[0], (n,), generator=g, device=DEV)
+        x = centres[u] + 0.4 * torch.randn(n, d, generator=g, device=DEV)
+        return (scale * x / x.norm(dim=1, keepdim=True)).to(
+            torch.float32 if dtype == "f32" else torch.bfloat16)
+    s = {"bank": rows(N), "queries": rows(B), "scales": None, "mask": None,
+         "qual": torch.rand(N, M, generator=g, device=DEV),
+         "len": torch.exp(5.0 + 0.6 * torch.randn(N, M, generator=g, device=DEV))}
+    if mask is not None:
+        live = torch.rand(N, generator=g, device=DEV) < 0.7
+        if mask == "all":
+            live[:] = False
+        elif N > 1:
+            live[0], live[N - 1] = False, True
+        s["mask"] = live.to(torch.uint8)
+    if dtype == "q4":
+        s["bank"], s["scales"], s["norms"] = rb.rb_bank_pack(s["bank"])
+        s["x"] = ref.unpack4(s["bank"], s["scales"])
+    else:
+        s["norms"] = rb.rb_bank_norms(s["bank"])
+        s["x"] = s["bank"].double()
+    if mask is not None:
+        dead = s["mask"] == 0
+        if dtype != "q4":
+            s["bank"][dead] = math.nan
+        s["norms"][dead] = math.nan
+        s["qual"][dead] = math.inf
+        s["len"][dead] = math.nan
+    g2 = torch.Generator(device=DEV).manual_seed(2000 + seed)
+    s["dq_hat"] = torch.randn(B, M, generator=g2, device=DEV)
+    s["dl_hat"] = torch.randn(B, M, generator=g2, device=DEV) * 1e-2
+    s["dlse"] = torch.randn(B, generator=g2, device=DEV)
+    return s
+
+
+def forward(s, beta, **kw):
+    import paper_2606_17949_amd as rb
+    return dict(zip(("q_hat", "l_hat", "lse"), rb.rb_attend(
+        s["queries"], s["bank"], s["norms"], beta, s["qual"], s["len"], scales=s["scales"],
+        row_mask=s["mask"], **kw)))
+
+
+def backward(s, beta, out, dlse=True, **kw):
+    import paper_2606_17949_amd as rb
+    return rb.rb_attend_backward(s["queries"], s["bank"], s["norms"], beta, s["qual"], s["len"],
+                                 out["q_hat"], out["l_hat"], out["lse"], s["dq_hat"], s["dl_hat"],
+                                 dlse=s["dlse"] if dlse else None, row_mask=s["mask"], **kw)
+
+
+def dirty(nbytes):
+    return torch.full((max(nbytes, 256),), 0xff, dtype=torch.uint8, device=DEV)
+
+
+SIZES = [
+    # B, N, d (f32, bf16, q4), M, beta: one row, one request, rows and requests
+    # that end inside every tile, labels of one to more than two tiles of columns
+    (1, 1, (4, 8, 32), 1, 8.0), (1, 2, (12, 24, 32), 4, 1e-3), (2, 31, (100, 104, 96), 3, 4.0),
+    (3, 33, (64, 64, 64), 8, 30.0), (16, 257, (20, 40, 160), 9, 2.0),
+    (17, 1000, (384, 384, 384), 16, 8.0), (33, 2049, (300, 200, 544), 17, 16.0),
+    (64, 5001, (768, 768, 768), 4, 8.0), (65, 3000, (132, 136, 128), 5, 50.0),
+    (130, 700, (516, 1000, 1024), 33, 3.0), (70, 1300, (2048, 2048, 2048), 4, 8.0),
+    (200, 20_011, (96, 128, 128), 2, 6.0),
+]
+
+
+@pytest.mark.parametrize("mask", [None, "some"])
+@pytest.mark.parametrize("B,N,d,M,beta", SIZES)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "q4"])
+def test_forward_and_usage(dtype, B, N, d, M, beta, mask):
+    import paper_2606_17949_amd as rb
+    d = d[("f32", "bf16", "q4").index(dtype)]
+    label = f"{dtype} B={B} N={N} d={d} M={M} beta={beta} mask={mask}"
+    print(label, flush=True)
+    s = make(dtype, B, N, d, M, seed=N + B, mask=mask)
+    code = {"f32": rb.RB_F32, "bf16": rb.RB_BF16, "q4": rb.RB_Q4}[dtype]
+    out = forward(s, beta, ws=dirty(rb.rb_attend_workspace_size(B, N, d, code, M)))
+    torch.cuda.synchronize()
+    for k, (value, bound) in ref.attend(s["queries"], s["x"], beta, s["qual"], s["len"],
+                                        s["mask"]).items():
+        print(k, ref.check(k, out[k], value, bound, label), flush=True)
+    old = torch.rand(N, device=DEV)
+    use = old.clone()
+    rb.rb_attend_usage(s["queries"], s["bank"], s["norms"], beta, out["lse"], use, decay=0.75,
+                       scales=s["scales"], row_mask=s["mask"],
+                       ws=dirty(rb.rb_attend_usage_workspace_size(B, N, d, code)))
+    torch.cuda.synchronize()
+    value, bound = ref.usage(s["queries"], s["x"], beta, out["lse"], old, 0.75, s["mask"])
+    print("usage", ref.check("usage", use, value, bound, label), flush=True)
+
+
+@pytest.mark.parametrize("mask", [None, "some"])
+@pytest.mark.parametrize("B,N,d,M,beta", SIZES)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_backward(dtype, B, N, d, M, beta, mask):
+    import paper_2606_17949_amd as rb
+    d = d[("f32", "bf16").index(dtype)]
+    label = f"{dtype} B={B} N={N} d={d} M={M} beta={beta} mask={mask}"
+    print(label, flush=True)
+    s = make(dtype, B, N, d, M, seed=N + B, mask=mask)
+    code = rb.RB_F32 if dtype == "f32" else rb.RB_BF16
+    out = forward(s, beta)
+    got = backward(s, beta, out,
+                   ws=dirty(rb.rb_attend_backward_workspace_size(B, N, d, code, M)))
+    torch.cuda.synchronize()
+    want = ref.backward(s["queries"], s["x"], beta, s["qual"], s["len"], out["q_hat"],
+                        out["l_hat"], out["lse"], s["dq_hat"], s["dl_hat"], s["dlse"], s["mask"])
+    for k, (value, bound) in want.items():
+        half = torch.finfo(got[k].dtype).eps / 2
+        print(k, ref.check(k, got[k], value, bound + half * value.abs() + ref.T, label),
+              flush=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "q4"])
+def test_no_row_left(dtype):
+    """Every row masked: no prediction, lse -inf, nothing added to any gradient."""
+    import paper_2606_17949_amd as rb
+    s = make(dtype, 5, 100, 64, 3, mask="all")
+    out = forward(s, 4.0)
+    assert torch.isnan(out["q_hat"]).all() and torch.isnan(out["l_hat"]).all()
+    assert torch.isneginf(out["lse"]).all()
+    use = torch.rand(100, device=DEV)
+    was = use.clone()
+    rb.rb_attend_usage(s["queries"], s["bank"], s["norms"], 4.0, out["lse"], use, decay=0.5,
+                       scales=s["scales"], row_mask=s["mask"])
+    assert torch.equal(use, was * 0.5)
+    if dtype == "q4":
+        return
+    s["dq_hat"][:] = math.nan   # (what a loss over no numbers would give)
+    for k, v in backward(s, 4.0, out).items():
+        assert torch.count_nonzero(v) == 0, k
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_some_requests_dead(dtype):
+    """A request without weights among others (lse -inf given) adds nothing."""
+    s = make(dtype, 20, 300, 64, 3)
+    out = forward(s, 4.0)
+    whole = backward(s, 4.0, out)
+    dead = torch.zeros(20, dtype=torch.bool, device=DEV)
+    dead[[0, 7, 19]] = True
+    out["lse"][dead] = -math.inf
+    out["q_hat"][dead] = math.nan
+    s["dl_hat"][dead] = math.nan
+    got = backward(s, 4.0, out)
+    want = ref.backward(s["queries"], s["x"], 4.0, s["qual"], s["len"], out["q_hat"],
+                        out["l_hat"], out["lse"], s["dq_hat"], s["dl_hat"], s["dlse"])
+    for k, (value, bound) in want.items():
+        half = torch.finfo(got[k].dtype).eps / 2
+        ref.check(k, got[k], value, bound + half * value.abs() + ref.T)
+    assert torch.equal(got["d_queries"][~dead], whole["d_queries"][~dead])
+    assert torch.count_nonzero(got["d_queries"][dead]) == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "q4"])
+@pytest.mark.parametrize("beta,scale", [(1e4, 1.0), (1.0, 100.0), (1e-30, 1.0), (1e-3, 1e-3)])
+def test_far_and_flat(dtype, beta, scale):
+    """Scores of tens of thousands (all weight on the nearest rows) and of next to nothing."""
+    s = make(dtype, 9, 400, 96, 4, scale=scale)
+    out = forward(s, beta)
+    for k, (value, bound) in ref.attend(s["queries"], s["x"], beta, s["qual"], s["len"]).items():
+        print(k, ref.check(k, out[k], value, bound, f"{dtype} {beta} {scale}"), flush=True)
+
+
+def test_maximum_rises_late():
+    """The nearest rows come last, each nearer than all before it."""
+    N, d = 3000, 64
+    s = make("bf16", 4, N, d, 2)
+    q = s["queries"][:1].float()
+    t = torch.linspace(1.0, 0.0, N, device=DEV)[:, None]
+    s["bank"] = (q + 4.0 * t * torch.ones(1, d, device=DEV)).bfloat16()
+    s["queries"] = q.expand(4, d).bfloat16().contiguous()
+    import paper_2606_17949_amd as rb
+    s["norms"] = rb.rb_bank_norms(s["bank"])
+    s["x"] = s["bank"].double()
+    out = forward(s, 3.0)
+    for k, (value, bound) in ref.attend(s["queries"], s["x"], 3.0, s["qual"], s["len"]).items():
+        print(k, ref.check(k, out[k], value, bound), flush=True)
+
+
+@pytest.mark.parametrize("wanted", [("d_queries",), ("d_bank",), ("d_qual",), ("d_len",),
+                                    ("d_beta",), ("d_queries", "d_len"), ("d_bank", "d_beta")])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_single_gradients(dtype, wanted):
+    """Each output alone is bit for bit what it is among all; the others stay untouched."""
+    s = make(dtype, 70, 900, 128, 5, mask="some")
+    out = forward(s, 4.0)
+    whole = backward(s, 4.0, out)
+    some = backward(s, 4.0, out, **{k: torch.full_like(whole[k], 7.0) for k in wanted})
+    assert set(some) == set(wanted)
+    for k in wanted:
+        assert torch.equal(some[k], whole[k]), k
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients_against_differences(dtype):
+    """The sum of the gradients along a direction is the loss's difference along it
+    (of the 64-bit forward pass), for requests, rows, labels and beta."""
+    s = make(dtype, 6, 150, 32, 3)
+    beta = 2.5
+    out = forward(s, beta)
+    got = backward(s, beta, out)
+    g = torch.Generator(device=DEV).manual_seed(5)
+
+    def loss(q, x, b, qual, length):
+        score = -b * torch.cdist(q, x, compute_mode="donot_use_mm_for_euclid_dist") ** 2
+        p = torch.softmax(score, 1)
+        return float(((p @ qual) * s["dq_hat"].double()).sum() +
+                     ((p @ length) * s["dl_hat"].double()).sum() +
+                     (torch.logsumexp(score, 1) * s["dlse"].double()).sum())
+    at = [s["queries"].double(), s["x"], torch.tensor(beta, dtype=torch.float64, device=DEV),
+          s["qual"].double(), s["len"].double()]
+    grads = [got["d_queries"].double(), got["d_bank"].double(), got["d_beta"].double().sum(),
+             got["d_qual"].double(), got["d_len"].double()]
+    h = 1e-5
+    for i, name in enumerate(("queries", "bank", "beta", "qual", "len")):
+        v = torch.randn(at[i].shape, generator=g, device=DEV, dtype=torch.float64)
+        up, down = list(at), list(at)
+        up[i], down[i] = at[i] + h * v, at[i] - h * v
+        slope = (loss(*up) - loss(*down)) / (2 * h)
+        along = float((grads[i] * v).sum())
+        # the outputs' roundings along v (independent, half a step each at most),
+        # 32-bit weights and sums (1e-5 of the terms), the difference's own error
+        # (h^2 times a third derivative, 64-bit cancellation)
+        terms = float((grads[i] * v).abs().sum())
+        step = torch.finfo(s["queries"].dtype).eps / 2 if i < 2 else U32
+        tol = 4.0 * step * float((grads[i] * v).norm()) + 1e-5 * terms + 1e-6 * (1 + terms)
+        print(name, slope, along, tol, flush=True)
+        assert abs(slope - along) <= tol, name
+
+
+U32 = 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "q4"])
+def test_same_bits_every_time(dtype):
+    import paper_2606_17949_amd as rb
+    s = make(dtype, 150, 4000, 256, 4, mask="some")
+    first = forward(s, 5.0)
+    use = torch.zeros(4000, device=DEV)
+    rb.rb_attend_usage(s["queries"], s["bank"], s["norms"], 5.0, first["lse"], use,
+                       scales=s["scales"], row_mask=s["mask"])
+    grads = backward(s, 5.0, first) if dtype != "q4" else {}
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        with torch.cuda.stream(other):
+            again = forward(s, 5.0)
+            use2 = torch.zeros(4000, device=DEV)
+            rb.rb_attend_usage(s["queries"], s["bank"], s["norms"], 5.0, again["lse"], use2,
+                               scales=s["scales"], row_mask=s["mask"])
+            grads2 = backward(s, 5.0, again) if dtype != "q4" else {}
+        other.synchronize()
+        for k in first:
+            assert torch.equal(first[k], again[k]), k
+        assert torch.equal(use, use2)
+        for k in grads:
+            assert torch.equal(grads[k], grads2[k]), k
+
+
+def test_rows_behind_the_outputs_stay():
+    """Outputs in the middle of larger buffers: nothing around them is written."""
+    import paper_2606_17949_amd as rb
+    B, N, d, M = 19, 333, 72, 5
+    for dtype in ("f32", "bf16"):
+        s = make(dtype, B, N, d, M)
+        dt = s["queries"].dtype
+        bufs = {}
+
+        def place(name, n, dtype_):
+            buf = torch.full((n + 128,), 3.0, dtype=dtype_, device=DEV)
+            bufs[name] = (buf, n)
+            return buf[64:64 + n]
+        out = {"q_hat": place("q_hat", B * M, torch.float32).view(B, M),
+               "l_hat": place("l_hat", B * M, torch.float32).view(B, M),
+               "lse": place("lse", B, torch.float32)}
+        forward(s, 3.0, **out)
+        backward(s, 3.0, out, d_queries=place("d_queries", B * d, dt).view(B, d),
+                 d_bank=place("d_bank", N * d, dt).view(N, d),
+                 d_qual=place("d_qual", N * M, torch.float32).view(N, M),
+                 d_len=place("d_len", N * M, torch.float32).view(N, M),
+                 d_beta=place("d_beta", B, torch.float32))
+        use = place("usage", N, torch.float32)
+        rb.rb_attend_usage(s["queries"], s["bank"], s["norms"], 3.0, out["lse"], use)
+        torch.cuda.synchronize()
+        for k, (buf, n) in bufs.items():
+            assert (buf[:64] == 3.0).all() and (buf[64 + n:] == 3.0).all(), k
+
+
+def test_empty_batch():
+    import paper_2606_17949_amd as rb
+    s = make("f32", 2, 50, 16, 3)
+    q = s["queries"][:0]
+    e = torch.empty(0, 3, device=DEV)
+    q_hat, l_hat, lse = rb.rb_attend(q, s["bank"], s["norms"], 2.0, s["qual"], s["len"])
+    assert q_hat.shape == (0, 3) and lse.shape == (0,)
+    use = torch.ones(50, device=DEV)
+    rb.rb_attend_usage(q, s["bank"], s["norms"], 2.0, lse, use, decay=0.25)
+    assert (use == 0.25).all()
+    got = rb.rb_attend_backward(q, s["bank"], s["norms"], 2.0, s["qual"], s["len"], e, e, lse, e, e)
+    for k in ("d_bank", "d_qual", "d_len"):
+        assert torch.count_nonzero(got[k]) == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "q4"])
+def test_captured_and_replayed(dtype):
+    """Forward, usage and gradients in one graph, replayed on new requests with
+    eager work in between, equal the eager calls bit for bit."""
+    import paper_2606_17949_amd as rb
+    B, N, d, M = 40, 1500, 128, 4
+    s = make(dtype, B, N, d, M, mask="some")
+    code = {"f32": rb.RB_F32, "bf16": rb.RB_BF16, "q4": rb.RB_Q4}[dtype]
+    other = make(dtype, B, N, d, M, seed=9)
+    keep = {"ws": rb.attend_workspace(B, N, d, code, M), "q_hat": torch.empty(B, M, device=DEV),
+            "l_hat": torch.empty(B, M, device=DEV), "lse": torch.empty(B, device=DEV)}
+    uws = rb.attend_usage_workspace(B, N, d, code)
+    use = torch.zeros(N, device=DEV)
+    grads = {}
+    if dtype != "q4":
+        gws = rb.attend_backward_workspace(B, N, d, code, M)
+        grads = {"d_queries": torch.empty_like(s["queries"]), "d_bank": torch.empty_like(s["bank"]),
+                 "d_qual": torch.empty(N, M, device=DEV), "d_len": torch.empty(N, M, device=DEV),
+                 "d_beta": torch.empty(B, device=DEV)}
+
+    def step():
+        forward(s, 5.0, **keep)
+        rb.rb_attend_usage(s["queries"], s["bank"], s["norms"], 5.0, keep["lse"], use, decay=0.5,
+                           scales=s["scales"], row_mask=s["mask"], ws=uws)
+        if grads:
+            backward(s, 5.0, keep, ws=gws, **grads)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(3):
+        s["queries"].copy_(other["queries"].roll(k, 0))
+        use.fill_(1.0 + k)
+        graph.replay()
+        torch.cuda.synchronize()
+        seen = {n: t.clone() for n, t in {**keep, **grads, "usage": use}.items() if n != "ws"}
+        use.fill_(1.0 + k)
+        step()
+        torch.cuda.synchronize()
+        for n, t in seen.items():
+            now = {**keep, **grads, "usage": use}[n]
+            assert torch.equal(t, now), (k, n)
