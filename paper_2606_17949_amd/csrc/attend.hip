@@ -7,7 +7,11 @@ namespace rb {
 
 namespace {
 
-constexpr int AT_RING = 6;       // k-steps of bank rows in flight
+// k-steps of bank rows in flight (4-bit rows: 128 elements each)
+constexpr int at_ring(int dt, int rt) { return dt == AT_Q4 || rt == 4 ? 2 : 4; }
+// 16-row tiles of a slab: 64 requests read each fragment of theirs from LDS for
+// 64 rows; with 32, LDS reads alone take as long as the products.
+constexpr int at_rt(int dt, int ng) { return dt != AT_F32 && ng == 4 ? 4 : 2; }
 // A running maximum is raised when a score passes it by this many powers of
 // two: weights stay below 2^16 and few slabs rescale what went before.
 constexpr float AT_SLACK = 16.f;
@@ -30,7 +34,7 @@ struct AttendArgs {
 //            MFMA (fp32, 16 label columns x 16 requests, 4 rows): its operand
 //            p[row 4*(lane/16) + e][request lane%16] is register e of the
 //            scores as it stands.
-template <int DT, int NG, int CT>
+template <int DT, int NG, int RT, int CT>
 __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const AttendArgs A)
 {
     extern __shared__ __align__(16) uint8_t smem[];
@@ -84,51 +88,62 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
             o[g][k] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // norms, mask and labels of a slab: this lane's rows 16*r + 4*jg + e
-    f32x4 nh[AT_RT];             // -|x|^2/2, -inf for rows masked or past the bank
-    float v[AT_RT][4][CT];
-    auto side = [&](long slab) {
-        const long r0 = slab * AT_SLAB + jg * 4;
+    // norms, mask and labels of a slab: this lane's rows 16*r + 4*jg + e (the
+    // last row again for those past the bank)
+    float nrm[RT][4], v[RT][4][CT];
+    // four rows' mask bytes lie in one or two aligned words
+    uint32_t mk[RT][2];
+    const bool masked = A.b.mask != nullptr;
+    const uint32_t *const mask4 = (const uint32_t *)((uintptr_t)A.b.mask & ~(uintptr_t)3);
+    const uint32_t mask_sh = (uint32_t)((uintptr_t)A.b.mask & 3);
+    const size_t mask_last = ((size_t)N - 1 + mask_sh) / 4;
+    auto side = [&](int slab) {
+        const long r0 = (s0 + slab) * (16 * RT) + jg * 4;
 #pragma unroll
-        for (int r = 0; r < AT_RT; ++r)
+        for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const long row = r0 + r * 16 + e;
-                const bool in = row < N;
-                const size_t at = in ? (size_t)row : 0;
-                const bool ok = in && (!A.b.mask || A.b.mask[at] != 0);
-                nh[r][e] = ok ? -0.5f * A.b.norms[at] : -INFINITY;
+                const size_t at = (size_t)min(r0 + r * 16 + e, (long)N - 1);
+                nrm[r][e] = A.b.norms[at];
 #pragma unroll
-                for (int k = 0; k < CT; ++k) {
-                    const float x = lab[k][at * A.M];
-                    v[r][e][k] = ok && lab_ok[k] ? x : 0.f;
-                }
+                for (int k = 0; k < CT; ++k)
+                    v[r][e][k] = lab[k][at * A.M];
+            }
+        if (masked)
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const size_t w = (size_t)(r0 + r * 16) / 4;
+                mk[r][0] = mask4[min(w, mask_last)];
+                mk[r][1] = mask4[min(w + 1, mask_last)];
             }
     };
-    auto start = [&](int slab, f32x4(&acc)[AT_RT][NG]) {
-        side(min(s0 + slab, A.slabs - 1));
+    auto end = [&](int slab, f32x4(&acc)[RT][NG]) {
+        const long r0 = (s0 + slab) * (16 * RT) + jg * 4;
+        __builtin_amdgcn_sched_barrier(0);
+        // scores: -inf for rows masked or past the bank, whatever they hold
 #pragma unroll
-        for (int r = 0; r < AT_RT; ++r)
+        for (int r = 0; r < RT; ++r) {
+            const uint32_t four =
+                masked ? __builtin_amdgcn_alignbyte(mk[r][1], mk[r][0], mask_sh) : ~0u;
 #pragma unroll
-            for (int g = 0; g < NG; ++g)
+            for (int e = 0; e < 4; ++e) {
+                const bool ok = r0 + r * 16 + e < N && (four >> (8 * e) & 0xffu) != 0;
+                const float nh = -0.5f * nrm[r][e];
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    acc[r][g][e] = nh[r][e] + hq[g];
-    };
-    auto end = [&](int, f32x4(&acc)[AT_RT][NG]) {
+                for (int k = 0; k < CT; ++k)
+                    v[r][e][k] = ok && lab_ok[k] ? v[r][e][k] : 0.f;
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+                    acc[r][g][e] = ok ? acc[r][g][e] + (nh + hq[g]) : -INFINITY;
+            }
+        }
         bool raise = false;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
             float m = -INFINITY;
 #pragma unroll
-            for (int r = 0; r < AT_RT; ++r)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    // (a masked row may hold anything)
-                    if (A.b.mask)
-                        acc[r][g][e] = nh[r][e] == -INFINITY ? -INFINITY : acc[r][g][e];
-                    m = fmaxf(m, acc[r][g][e]);
-                }
+            for (int r = 0; r < RT; ++r)
+                m = fmaxf(m, max4(acc[r][g]));
             raise |= c * m > ref[g] + AT_SLACK;
         }
         if (ballot(raise)) {
@@ -136,7 +151,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
             for (int g = 0; g < NG; ++g) {
                 float m = -INFINITY;
 #pragma unroll
-                for (int r = 0; r < AT_RT; ++r)
+                for (int r = 0; r < RT; ++r)
                     m = fmaxf(m, max4(acc[r][g]));
                 m = rows_reduce(c * m, [](float x, float y) { return fmaxf(x, y); });
                 const float up = fmaxf(ref[g], m);
@@ -149,22 +164,25 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
                     o[g][k] *= f;
             }
         }
+        // (no instruction moves across a row's bounds, which keeps few weights live)
 #pragma unroll
-        for (int r = 0; r < AT_RT; ++r)
+        for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < 4; ++e) {
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
-                    const float p =
-                        __builtin_amdgcn_exp2f(fmaf(c, acc[r][g][e], -sub[g]));
+                    const float p = __builtin_amdgcn_exp2f(fmaf(c, acc[r][g][e], -sub[g]));
                     l[g] += p;
 #pragma unroll
                     for (int k = 0; k < CT; ++k)
                         o[g][k] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[r][e][k], p, o[g][k], 0,
                                                                       0, 0);
                 }
+            }
+        __builtin_amdgcn_sched_barrier(0);
     };
-    scan_slabs<DT, NG, AT_RING, false>(A.b, A.nks, qs, s0, s1, lane, start, end);
+    scan_slabs<DT, NG, RT, at_ring(DT, RT), false>(A.b, A.nks, qs, s0, s1, lane, side, end);
 
     // ---- the waves' sums, joined (the request tile's LDS is free now)
     constexpr int W = 2 + 16 * CT;
@@ -278,10 +296,10 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const float *ml, const
     }
 }
 
-template <int DT, int NG, int CT>
+template <int DT, int NG, int RT, int CT>
 hipError_t launch_one(const AttendPlan &p, const AttendArgs &a, hipStream_t s)
 {
-    auto kern = attend_kernel<DT, NG, CT>;
+    auto kern = attend_kernel<DT, NG, RT, CT>;
     const hipError_t e = hipFuncSetAttribute(
         (const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.lds_bytes);
     if (e != hipSuccess)
@@ -295,9 +313,9 @@ template <int DT, int CT>
 hipError_t launch_ng(const AttendPlan &p, const AttendArgs &a, hipStream_t s)
 {
     switch (p.ng) {
-    case 1: return launch_one<DT, 1, CT>(p, a, s);
-    case 2: return launch_one<DT, 2, CT>(p, a, s);
-    case 4: return launch_one<DT, 4, CT>(p, a, s);
+    case 1: return launch_one<DT, 1, 2, CT>(p, a, s);
+    case 2: return launch_one<DT, 2, 2, CT>(p, a, s);
+    case 4: return launch_one<DT, 4, at_rt(DT, 4), CT>(p, a, s);
     }
     return hipErrorInvalidValue;
 }
@@ -317,7 +335,6 @@ bool plan_attend(int B, int N, int d, int dtype, int M, int n_cu, AttendPlan *p)
     const int ks = at_ks(dtype);
     p->dtype = dtype;
     p->nks = (d + ks - 1) / ks;
-    p->slabs = (int)(((long)N + AT_SLAB - 1) / AT_SLAB);
     p->ct = 2 * M <= 16 ? 1 : 2;
     p->n_lt = (2 * M + 16 * p->ct - 1) / (16 * p->ct);
     const size_t group = (size_t)p->nks * ks * (dtype == AT_F32 ? 4 : 2) * 16;
@@ -327,13 +344,15 @@ bool plan_attend(int B, int N, int d, int dtype, int M, int n_cu, AttendPlan *p)
     if (group * ng > (size_t)AT_LDS)
         return false;
     p->ng = ng;
+    const int slab = 16 * at_rt(dtype, ng);
+    p->slabs = (int)(((long)N + slab - 1) / slab);
     p->n_qt = (B + ng * 16 - 1) / (ng * 16);
     // one workgroup per compute unit, as far as there are slabs for its waves;
     // a wave's part of the bank stays under 1 GB (32-bit offsets)
     const long tiles = (long)p->n_qt * p->n_lt;
     long chunks = n_cu / tiles;
     const long by_size =
-        ((long)p->slabs * AT_SLAB * at_row_bytes(dtype, d) >> 30) / AT_WAVES + 1;
+        ((long)p->slabs * slab * at_row_bytes(dtype, d) >> 30) / AT_WAVES + 1;
     if (chunks < by_size)
         chunks = by_size;
     if (chunks > p->slabs)

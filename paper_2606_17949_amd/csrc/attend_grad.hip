@@ -8,7 +8,11 @@ namespace rb {
 
 namespace {
 
-constexpr int AT_RING = 6;             // k-steps of bank rows in flight
+// k-steps of bank rows in flight (4-bit rows: 128 elements each)
+constexpr int at_ring(int dt, int rt) { return dt == AT_Q4 || rt == 4 ? 2 : 4; }
+// 16-row tiles of a slab: 64 requests read each fragment of theirs from LDS for
+// 64 rows; with 32, LDS reads alone take as long as the products.
+constexpr int at_rt(int dt, int ng) { return dt != AT_F32 && ng == 4 ? 4 : 2; }
 constexpr size_t PART_BYTES = 128u << 20;   // ds of a part of the bank
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -72,7 +76,7 @@ struct UsageArgs {
 // Weights of the bank's rows: as the forward pass, with the bank's rows over
 // the lanes, so that a row's sum over the requests is a sum over registers and
 // four lanes. There is no running maximum: lse is known.
-template <int DT, int NG>
+template <int DT, int NG, int RT>
 __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_kernel(const UsageArgs A)
 {
     extern __shared__ __align__(16) uint8_t smem[];
@@ -106,35 +110,35 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_kernel(const UsageAr
             hq[g][e] = x.hq;
             lse2[g][e] = x.lse2;
         }
-    float nh[AT_RT];
-    auto start = [&](int slab, f32x4(&acc)[AT_RT][NG]) {
-        const long r0 = min(s0 + slab, A.slabs - 1) * AT_SLAB + col;
+    float nrm[RT];
+    uint8_t mk[RT];
+    const bool masked = A.b.mask != nullptr;
+    const uint8_t *const mask = masked ? A.b.mask : (const uint8_t *)A.b.norms;
+    auto side = [&](int slab) {
+        const long r0 = (s0 + slab) * (16 * RT) + col;
 #pragma unroll
-        for (int r = 0; r < AT_RT; ++r) {
-            const long row = r0 + r * 16;
-            const size_t at = row < N ? (size_t)row : 0;
-            const bool ok = row < N && (!A.b.mask || A.b.mask[at] != 0);
-            nh[r] = ok ? -0.5f * A.b.norms[at] : -INFINITY;
-#pragma unroll
-            for (int g = 0; g < NG; ++g)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    acc[r][g][e] = nh[r] + hq[g][e];
+        for (int r = 0; r < RT; ++r) {
+            const size_t at = (size_t)min(r0 + r * 16, (long)N - 1);
+            nrm[r] = A.b.norms[at];
+            mk[r] = mask[at];
         }
     };
-    auto end = [&](int slab, f32x4(&acc)[AT_RT][NG]) {
+    auto end = [&](int slab, f32x4(&acc)[RT][NG]) {
 #pragma unroll
-        for (int r = 0; r < AT_RT; ++r) {
+        for (int r = 0; r < RT; ++r) {
+            __builtin_amdgcn_sched_barrier(0);
+            const long row = (s0 + slab) * (16 * RT) + r * 16 + col;
+            const float nh = -0.5f * nrm[r];
             float sum = 0.f;
 #pragma unroll
             for (int g = 0; g < NG; ++g)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    sum += __builtin_amdgcn_exp2f(fmaf(c, acc[r][g][e], -lse2[g][e]));
+                    sum += __builtin_amdgcn_exp2f(
+                        fmaf(c, acc[r][g][e] + (nh + hq[g][e]), -lse2[g][e]));
             sum = rows_reduce(sum, [](float x, float y) { return x + y; });
-            if (nh[r] == -INFINITY)
+            if (masked && mk[r] == 0)
                 sum = 0.f;
-            const long row = (s0 + slab) * AT_SLAB + r * 16 + col;
             if (jg == 0 && row < N) {
                 if (A.part)
                     A.part[(size_t)t * N + row] = sum;
@@ -143,7 +147,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_kernel(const UsageAr
             }
         }
     };
-    scan_slabs<DT, NG, AT_RING, true>(A.b, A.nks, qs, s0, s1, lane, start, end);
+    scan_slabs<DT, NG, RT, at_ring(DT, RT), true>(A.b, A.nks, qs, s0, s1, lane, side, end);
 }
 
 __global__ __launch_bounds__(256) void usage_join_kernel(const float *part, int n_qt, int N,
@@ -251,23 +255,35 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_kernel(const DsArgs A)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             sum_ds[g][e] = sum_db[g][e] = 0.f;
-    float nh[AT_RT];
-    auto start = [&](int slab, f32x4(&acc)[AT_RT][NG]) {
-        const long r0 = min(s0 + slab, A.slab0 + A.slabs - 1) * AT_SLAB + col;
+    float nrm[AT_RT], vr[AT_RT][4];   // norms, mask, the first 16 label columns
+    uint8_t mk[AT_RT];
+    const bool masked = A.b.mask != nullptr;
+    const uint8_t *const mask = masked ? A.b.mask : (const uint8_t *)A.b.norms;
+    const float *lab[4];   // label column 4*j + jg
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int cc = 4 * j + jg;
+        lab[j] = cc < M ? A.qual + cc : cc < 2 * M ? A.len + (cc - M) : A.qual;
+    }
+    auto side = [&](int slab) {
+        const long r0 = (s0 + slab) * AT_SLAB + col;
 #pragma unroll
         for (int r = 0; r < AT_RT; ++r) {
-            const long row = r0 + r * 16;
-            const size_t at = row < N ? (size_t)row : 0;
-            const bool ok = row < N && (!A.b.mask || A.b.mask[at] != 0);
-            nh[r] = ok ? -0.5f * A.b.norms[at] : -INFINITY;
+            const size_t at = (size_t)min(r0 + r * 16, (long)N - 1);
+            nrm[r] = A.b.norms[at];
+            mk[r] = mask[at];
 #pragma unroll
-            for (int g = 0; g < NG; ++g)
-                acc[r][g] = side4(0, g) + nh[r];
+            for (int j = 0; j < 4; ++j)
+                vr[r][j] = lab[j][at * M];
         }
     };
     const int n_ct = (2 * M + 15) / 16;
     auto end = [&](int slab, f32x4(&acc)[AT_RT][NG]) {
         const long row0 = (s0 + slab) * AT_SLAB + col;
+        float nh[AT_RT];   // -inf for rows masked or past the bank
+#pragma unroll
+        for (int r = 0; r < AT_RT; ++r)
+            nh[r] = row0 + r * 16 < N && !(masked && mk[r] == 0) ? -0.5f * nrm[r] : -INFINITY;
         // ---- dp: 4 label columns a step, request groups x row tiles
         f32x4 dp[AT_RT][NG];
 #pragma unroll
@@ -275,24 +291,38 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_kernel(const DsArgs A)
 #pragma unroll
             for (int g = 0; g < NG; ++g)
                 dp[r][g] = -side4(2, g);
-        for (int c0 = 0; c0 < 2 * M; c0 += 4) {
+        // (a masked row's labels may be no numbers)
+        auto dp_step = [&](int c0, float(&x)[AT_RT]) {
             const int cc = c0 + jg;
-            float v[AT_RT];
 #pragma unroll
-            for (int r = 0; r < AT_RT; ++r) {
-                const long row = row0 + r * 16;
-                const bool ok = nh[r] != -INFINITY && cc < 2 * M;
-                const size_t at = ok ? (size_t)row * M + (cc < M ? cc : cc - M) : 0;
-                const float x = (cc < M ? A.qual : A.len)[at];
-                v[r] = ok ? x : 0.f;   // (a masked row's labels may be no numbers)
-            }
+            for (int r = 0; r < AT_RT; ++r)
+                x[r] = nh[r] != -INFINITY && cc < 2 * M ? x[r] : 0.f;
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 const float a = dout(g * 16 + col, cc);
 #pragma unroll
                 for (int r = 0; r < AT_RT; ++r)
-                    dp[r][g] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, v[r], dp[r][g], 0, 0, 0);
+                    dp[r][g] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, x[r], dp[r][g], 0, 0, 0);
             }
+        };
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (4 * j < 2 * M) {
+                float x[AT_RT];
+#pragma unroll
+                for (int r = 0; r < AT_RT; ++r)
+                    x[r] = vr[r][j];
+                dp_step(4 * j, x);
+            }
+        for (int c0 = 16; c0 < 2 * M; c0 += 4) {
+            const int cc = c0 + jg;
+            float x[AT_RT];
+#pragma unroll
+            for (int r = 0; r < AT_RT; ++r) {
+                const size_t at = (size_t)min(row0 + r * 16, (long)N - 1) * M;
+                x[r] = cc < M ? A.qual[at + cc] : cc < 2 * M ? A.len[at + cc - M] : 0.f;
+            }
+            dp_step(c0, x);
         }
         // ---- p in place of the scores, ds in place of dp
         float rs[AT_RT];
@@ -303,11 +333,11 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_kernel(const DsArgs A)
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 __builtin_amdgcn_sched_barrier(0);
-                const f32x4 lse2 = side4(1, g);
+                const f32x4 hq = side4(0, g), lse2 = side4(1, g);
                 float hi[4], lo[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float a = live ? acc[r][g][e] : 0.f;
+                    const float a = live ? acc[r][g][e] + (nh[r] + hq[e]) : 0.f;
                     const float p =
                         live ? __builtin_amdgcn_exp2f(fmaf(c, a, -lse2[e])) : 0.f;
                     const float ds = p * dp[r][g][e];
@@ -403,7 +433,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_kernel(const DsArgs A)
             }
         }
     };
-    scan_slabs<DT, NG, AT_RING, true>(A.b, A.nks, qs, s0, s1, lane, start, end);
+    scan_slabs<DT, NG, AT_RT, at_ring(DT, AT_RT), true>(A.b, A.nks, qs, s0, s1, lane, side, end);
 
     // ---- the requests' sums, joined over the waves
     float *jn = (float *)smem;   // [n_waves][NG * 16][2]
@@ -817,10 +847,10 @@ hipError_t allow_lds(K kern, size_t bytes)
                                (int)bytes);
 }
 
-template <int DT, int NG>
+template <int DT, int NG, int RT>
 hipError_t usage_one(const UsagePlan &p, const UsageArgs &a, hipStream_t s)
 {
-    auto kern = usage_kernel<DT, NG>;
+    auto kern = usage_kernel<DT, NG, RT>;
     const hipError_t e = allow_lds(kern, p.lds_bytes);
     if (e != hipSuccess)
         return e;
@@ -832,9 +862,9 @@ template <int DT>
 hipError_t usage_dt(const UsagePlan &p, const UsageArgs &a, hipStream_t s)
 {
     switch (p.ng) {
-    case 1: return usage_one<DT, 1>(p, a, s);
-    case 2: return usage_one<DT, 2>(p, a, s);
-    case 4: return usage_one<DT, 4>(p, a, s);
+    case 1: return usage_one<DT, 1, 2>(p, a, s);
+    case 2: return usage_one<DT, 2, 2>(p, a, s);
+    case 4: return usage_one<DT, 4, at_rt(DT, 4)>(p, a, s);
     }
     return hipErrorInvalidValue;
 }
@@ -863,10 +893,10 @@ hipError_t ds_dt(const GradPlan &p, const DsArgs &a, hipStream_t s)
 
 // Shares of `slabs` slabs for n_qt request tiles: about one workgroup per
 // compute unit, a wave's part of the bank under 1 GB.
-void shares(int slabs, int dtype, int d, int n_qt, int n_cu, int *n_chunks, int *waves)
+void shares(int slabs, int slab, int dtype, int d, int n_qt, int n_cu, int *n_chunks, int *waves)
 {
     long chunks = n_cu / n_qt;
-    const long by_size = ((long)slabs * AT_SLAB * at_row_bytes(dtype, d) >> 30) / AT_WAVES + 1;
+    const long by_size = ((long)slabs * slab * at_row_bytes(dtype, d) >> 30) / AT_WAVES + 1;
     if (chunks < by_size)
         chunks = by_size;
     if (chunks > slabs)
@@ -993,7 +1023,6 @@ bool plan_usage(int B, int N, int d, int dtype, int n_cu, UsagePlan *p)
     const int ks = at_ks(dtype);
     p->dtype = dtype;
     p->nks = (d + ks - 1) / ks;
-    p->slabs = (int)(((long)N + AT_SLAB - 1) / AT_SLAB);
     const size_t group = (size_t)p->nks * ks * (dtype == AT_F32 ? 4 : 2) * 16 + 16 * sizeof(Side);
     int ng = B <= 16 ? 1 : B <= 32 ? 2 : 4;
     while (ng > 1 && group * ng > (size_t)AT_LDS)
@@ -1001,8 +1030,10 @@ bool plan_usage(int B, int N, int d, int dtype, int n_cu, UsagePlan *p)
     if (group * ng > (size_t)AT_LDS)
         return false;
     p->ng = ng;
+    const int slab = 16 * at_rt(dtype, ng);
+    p->slabs = (int)(((long)N + slab - 1) / slab);
     p->n_qt = (B + ng * 16 - 1) / (ng * 16);
-    shares(p->slabs, dtype, d, p->n_qt, n_cu, &p->n_chunks, &p->waves);
+    shares(p->slabs, slab, dtype, d, p->n_qt, n_cu, &p->n_chunks, &p->waves);
     p->lds_bytes = group * ng;
     p->off_side = 0;
     p->off_part = up256((size_t)B * sizeof(Side));
@@ -1084,7 +1115,7 @@ bool plan_grad(int B, int N, int d, int dtype, int M, int n_cu, GradPlan *p)
     const int n_parts = (int)((p->slabs + part - 1) / part);
     part = (p->slabs + n_parts - 1) / n_parts;
     p->part_slabs = (int)part;
-    shares((int)part, dtype, d, p->n_qt, n_cu, &p->n_chunks, &p->waves);
+    shares((int)part, AT_SLAB, dtype, d, p->n_qt, n_cu, &p->n_chunks, &p->waves);
     const long tiles = (long)((d + DQ_COLS - 1) / DQ_COLS) *
                        ((B + DQ_GROUPS * 16 - 1) / (DQ_GROUPS * 16));
     long qc = n_cu / tiles;
