@@ -430,7 +430,8 @@ rb_status rb_attend(const void *queries, const void *bank, const uint8_t *scales
  * gradients of 0. Outputs are overwritten, and must not overlap the inputs. The
  * norms are taken as functions of the rows. dtype is RB_F32 or RB_BF16. For
  * bf16, ds enters the two products over d as a sum of two bf16 values (17 bits).
- * d_queries, d_bank 16-byte aligned. */
+ * d_queries, d_bank 16-byte aligned. Batches whose requests, B and d rounded up
+ * to multiples of 32, reach 2 GB are refused with RB_ERR_DIMS. */
 rb_status rb_attend_backward_workspace_size(int B, int N, int d, rb_dtype dtype, int M,
                                             size_t *bytes);
 rb_status rb_attend_backward(const void *queries, const void *bank, const float *bank_norms,

@@ -54,18 +54,17 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
     const float c = A.b.c;
 
     load_requests<DT, NG>(A.b, A.nks, q0, qs, wave, n_waves, lane);
-    wait_vmcnt<0>();
-    stream_barrier();
-
-    // -|q|^2/2 of this lane's requests, from the fragments in LDS
+    // once it is there: -|q|^2/2 of this lane's requests
     float hq[NG];
+    auto ready = [&] {
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-        float sum = 0.f;
-        for (int f = 0; f < A.nks * AtElem<DT>::SUB; ++f)
-            sum = sumsq16<DT == AT_F32 ? 0 : 1>(qs[(f * NG + g) * WAVE + lane], sum);
-        hq[g] = -0.5f * rows_reduce(sum, [](float x, float y) { return x + y; });
-    }
+        for (int g = 0; g < NG; ++g) {
+            float sum = 0.f;
+            for (int f = 0; f < A.nks * AtElem<DT>::SUB; ++f)
+                sum = sumsq16<DT == AT_F32 ? 0 : 1>(qs[(f * NG + g) * WAVE + lane], sum);
+            hq[g] = -0.5f * rows_reduce(sum, [](float x, float y) { return x + y; });
+        }
+    };
 
     // this lane's label columns
     const float *lab[CT];
@@ -182,7 +181,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
             }
         __builtin_amdgcn_sched_barrier(0);
     };
-    scan_slabs<DT, NG, RT, at_ring(DT, RT), false>(A.b, A.nks, qs, s0, s1, lane, side, end);
+    scan_slabs<DT, NG, RT, at_ring(DT, RT), false>(A.b, A.nks, qs, s0, s1, lane, ready, side, end);
 
     // ---- the waves' sums, joined (the request tile's LDS is free now)
     constexpr int W = 2 + 16 * CT;
@@ -225,64 +224,83 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
     }
 }
 
-// The shares' sums joined: one workgroup of 256 threads per request.
+// The shares' sums joined: one workgroup of 256 threads per request, 256 shares
+// at a time. What bounds it is latency: a share's maximum and sum, and the
+// columns (16 at a time, 16 shares side by side), are all sent for before the
+// first is used.
 __global__ __launch_bounds__(256) void attend_join_kernel(const float *ml, const float *o,
                                                           int n_chunks, int n_lt, int width, int B,
                                                           int M, float *q_hat, float *l_hat,
                                                           float *lse)
 {
-    __shared__ float red[256], wts[256];
-    const int b = blockIdx.x, tid = threadIdx.x;
-    float m = -INFINITY;
-    for (int ch = tid; ch < n_chunks; ch += 256)
-        m = fmaxf(m, ml[((size_t)ch * B + b) * 2]);
-    red[tid] = m;
-    __syncthreads();
-    for (int k = 128; k > 0; k >>= 1) {
-        if (tid < k)
-            red[tid] = fmaxf(red[tid], red[tid + k]);
+    __shared__ float red[256], wts[256], part[2][4];
+    const int b = blockIdx.x, tid = threadIdx.x, wave = tid >> 6;
+    const int col = tid & 15, row = tid >> 4;
+    // the block's maximum or sum of one value a thread
+    auto over = [&](int which, float v, auto op, float none) {
+        v = wave_reduce(v, op);
+        if ((tid & 63) == 0)
+            part[which][wave] = v;
         __syncthreads();
+        v = none;
+        for (int w = 0; w < 4; ++w)
+            v = op(v, part[which][w]);
+        return v;
+    };
+    auto pair = [&](int ch) {
+        return ch < n_chunks ? *(const f32x2 *)(ml + ((size_t)ch * B + b) * 2)
+                             : f32x2{-INFINITY, 0.f};
+    };
+    // column cc of 16 of the 256 shares from k0 on
+    auto columns = [&](int c0, int k0, float(&x)[16]) {
+        const int cc = c0 + col, tile = cc / width;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const int ch = k0 + k * 16 + row;
+            x[k] = cc < 2 * M && ch < n_chunks
+                       ? o[(((size_t)ch * n_lt + tile) * B + b) * width + cc - tile * width]
+                       : 0.f;
+        }
+    };
+    float x[16];
+    f32x2 mine = pair(tid);
+    columns(0, 0, x);
+    float m = mine[0];
+    for (int ch = tid + 256; ch < n_chunks; ch += 256)
+        m = fmaxf(m, pair(ch)[0]);
+    m = over(0, m, [](float u, float v) { return fmaxf(u, v); }, -INFINITY);
+    auto weight = [&](float v) {
+        return v == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(v - m);
+    };
+    float sum = weight(mine[0]) * mine[1];
+    wts[tid] = weight(mine[0]);
+    for (int ch = tid + 256; ch < n_chunks; ch += 256) {
+        const f32x2 p = pair(ch);
+        sum = fmaf(weight(p[0]), p[1], sum);
     }
-    m = red[0];
-    __syncthreads();
-    float sum = 0.f;
-    for (int ch = tid; ch < n_chunks; ch += 256) {
-        const float *at = ml + ((size_t)ch * B + b) * 2;
-        if (at[0] != -INFINITY)
-            sum = fmaf(__builtin_amdgcn_exp2f(at[0] - m), at[1], sum);
-    }
-    red[tid] = sum;
-    __syncthreads();
-    for (int k = 128; k > 0; k >>= 1) {
-        if (tid < k)
-            red[tid] += red[tid + k];
-        __syncthreads();
-    }
-    const float total = red[0];
+    const float total = over(1, sum, [](float u, float v) { return u + v; }, 0.f);
     if (tid == 0 && lse)
         lse[b] = (m + __builtin_amdgcn_logf(total)) * LN2;
-    // columns: 16 of them at a time, 16 shares side by side
-    const int col = tid & 15, part = tid >> 4;
     for (int c0 = 0; c0 < 2 * M; c0 += 16) {
-        const int cc = c0 + col, tile = cc / width;
         float s = 0.f;
         for (int k0 = 0; k0 < n_chunks; k0 += 256) {
-            __syncthreads();
-            const int ch = k0 + tid;
-            const float x = ch < n_chunks ? ml[((size_t)ch * B + b) * 2] : -INFINITY;
-            wts[tid] = x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - m);
-            __syncthreads();
-            if (cc < 2 * M)
-                for (int k = part; k < min(256, n_chunks - k0); k += 16)
-                    if (wts[k] != 0.f)
-                        s = fmaf(wts[k],
-                                 o[(((size_t)(k0 + k) * n_lt + tile) * B + b) * width + cc -
-                                   tile * width],
-                                 s);
+            if (n_chunks > 256) {
+                __syncthreads();
+                wts[tid] = weight(pair(k0 + tid)[0]);
+                __syncthreads();
+            }
+            if (c0 > 0 || k0 > 0)
+                columns(c0, k0, x);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const float w = wts[k * 16 + row];
+                s = w != 0.f ? fmaf(w, x[k], s) : s;
+            }
         }
         __syncthreads();
         red[tid] = s;
         __syncthreads();
+        const int cc = c0 + col;
         if (tid < 16 && cc < 2 * M) {
             s = 0.f;
             for (int k = 0; k < 16; ++k)

@@ -25,43 +25,102 @@ struct Side {
     float hq, lse2, shift, none;
 };
 
+struct PrepArgs {
+    const uint8_t *queries;
+    int B, d, M, pitch;
+    const float *lse, *q_hat, *l_hat, *dq, *dl, *dlse;
+    float *dout;     // [B][pitch] label gradients, 0 past 2 M; null: not wanted
+    Side *side;
+    int n_blk, n_dt; // fragments of the requests, [n_blk][n_dt][64]
+    i32x4 *qpack;
+};
+
 template <int QDT>
-__global__ __launch_bounds__(256) void side_kernel(const uint8_t *queries, int B, int d, int M,
-                                                   const float *lse, const float *q_hat,
-                                                   const float *l_hat, const float *dq,
-                                                   const float *dl, const float *dlse,
-                                                   float *dout, int pitch, Side *side)
+__device__ __forceinline__ void make_side(const PrepArgs &A, int b, int lane)
 {
-    const int lane = threadIdx.x & 63;
-    const int b = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (b >= B)
-        return;
-    const int n16 = d * Elem<QDT>::ESZ / 16;
-    const uint8_t *q = queries + (size_t)b * d * Elem<QDT>::ESZ;
+    const int n16 = A.d * Elem<QDT>::ESZ / 16;
+    const uint8_t *q = A.queries + (size_t)b * A.d * Elem<QDT>::ESZ;
     float s = 0.f;
     for (int i = lane; i < n16; i += WAVE)
         s = sumsq16<QDT>(load16(q + (size_t)i * 16), s);
     s = wave_sum(s);
-    const bool alive = lse[b] != -INFINITY;
+    const float lse = A.lse[b];
+    const bool alive = lse != -INFINITY;
     float dot = 0.f;
-    if (dout) {
+    if (A.dout) {
         // (a dead request's outputs are no numbers, and its gradients may be none)
-        for (int c = lane; c < pitch; c += WAVE) {
+        for (int c = lane; c < A.pitch; c += WAVE) {
             float g = 0.f, o = 0.f;
-            if (alive && c < 2 * M) {
-                const size_t at = (size_t)b * M + (c < M ? c : c - M);
-                g = c < M ? dq[at] : dl[at];
-                o = c < M ? q_hat[at] : l_hat[at];
+            if (alive && c < 2 * A.M) {
+                const size_t at = (size_t)b * A.M + (c < A.M ? c : c - A.M);
+                g = c < A.M ? A.dq[at] : A.dl[at];
+                o = c < A.M ? A.q_hat[at] : A.l_hat[at];
             }
             dot = fmaf(g, o, dot);
-            dout[(size_t)b * pitch + c] = g;
+            A.dout[(size_t)b * A.pitch + c] = g;
         }
         dot = wave_sum(dot);
-        if (alive && dlse)
-            dot -= dlse[b];
+        if (alive && A.dlse)
+            dot -= A.dlse[b];
     }
     if (lane == 0)
-        side[b] = Side{-0.5f * s, alive ? lse[b] * LOG2E : INFINITY, dot, 0.f};
+        A.side[b] = Side{-0.5f * s, alive ? lse * LOG2E : INFINITY, dot, 0.f};
+}
+
+// Fragments of the requests for d_bank: [block of requests][16 columns][64]
+// lanes, lane (column m = l % 16, requests 4*(l/16) .. of a group; bf16: of
+// two). Columns are dealt to pairs of fragments so that a lane's results of a
+// pair, m = 4*(l/16) + e of each, are eight that lie side by side.
+__device__ __forceinline__ int dealt_column(int dt, int m)
+{
+    return (dt >> 1) * 32 + (m >> 2) * 8 + (dt & 1) * 4 + (m & 3);
+}
+
+template <int QDT>
+__device__ __forceinline__ void make_qpack(const PrepArgs &A, long i)
+{
+    if (i >= (long)A.n_blk * A.n_dt * WAVE)
+        return;
+    const int lane = (int)(i % WAVE), dt = (int)(i / WAVE % A.n_dt),
+              blk = (int)(i / WAVE / A.n_dt);
+    const int cc = dealt_column(dt, lane & 15), jg = lane >> 4;
+    i32x4 r = i32x4{0, 0, 0, 0};
+    if (cc < A.d) {
+        if constexpr (QDT == 1) {
+            const uint16_t *q = (const uint16_t *)A.queries;
+            uint32_t v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int b = blk * 32 + (j >> 2) * 16 + 4 * jg + (j & 3);
+                v[j] = b < A.B ? q[(size_t)b * A.d + cc] : 0u;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                r[j] = (int)(v[2 * j] | (v[2 * j + 1] << 16));
+        } else {
+            const int *q = (const int *)A.queries;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int b = blk * 16 + 4 * jg + j;
+                r[j] = b < A.B ? q[(size_t)b * A.d + cc] : 0;
+            }
+        }
+    }
+    A.qpack[i] = r;
+}
+
+// What the other passes want of the requests, in one launch: four waves of one
+// request each, then blocks of fragments.
+template <int QDT>
+__global__ __launch_bounds__(256) void prep_kernel(const PrepArgs A, int side_blocks)
+{
+    if ((int)blockIdx.x < side_blocks) {
+        const int b = blockIdx.x * 4 + (threadIdx.x >> 6);
+        if (b < A.B)
+            make_side<QDT>(A, b, threadIdx.x & 63);
+    } else {
+        make_qpack<QDT>(A, (long)(blockIdx.x - side_blocks) * 256 + threadIdx.x);
+    }
 }
 
 struct UsageArgs {
@@ -98,18 +157,17 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_kernel(const UsageAr
     load_requests<DT, NG>(A.b, A.nks, q0, qs, wave, n_waves, lane);
     for (int i = tid; i < NG * 16; i += blockDim.x)
         sd[i] = q0 + i < A.b.B ? A.side[q0 + i] : Side{0.f, INFINITY, 0.f, 0.f};
-    wait_vmcnt<0>();
-    stream_barrier();
-
     float hq[NG][4], lse2[NG][4];
+    auto ready = [&] {
 #pragma unroll
-    for (int g = 0; g < NG; ++g)
+        for (int g = 0; g < NG; ++g)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const Side &x = sd[g * 16 + 4 * jg + e];
-            hq[g][e] = x.hq;
-            lse2[g][e] = x.lse2;
-        }
+            for (int e = 0; e < 4; ++e) {
+                const Side &x = sd[g * 16 + 4 * jg + e];
+                hq[g][e] = x.hq;
+                lse2[g][e] = x.lse2;
+            }
+    };
     float nrm[RT];
     uint8_t mk[RT];
     const bool masked = A.b.mask != nullptr;
@@ -147,7 +205,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_kernel(const UsageAr
             }
         }
     };
-    scan_slabs<DT, NG, RT, at_ring(DT, RT), true>(A.b, A.nks, qs, s0, s1, lane, side, end);
+    scan_slabs<DT, NG, RT, at_ring(DT, RT), true>(A.b, A.nks, qs, s0, s1, lane, ready, side, end);
 }
 
 __global__ __launch_bounds__(256) void usage_join_kernel(const float *part, int n_qt, int N,
@@ -194,7 +252,9 @@ struct DsArgs {
 
 // Where lane l (bank row l % 16, requests 4*(l/16) ..) of a fragment of ds has
 // its 16 bytes: rows turned by 4 for each four requests, so that reading it
-// across (four rows, 16 requests) meets every bank once.
+// across (four rows, 16 requests) meets every bank once. The two halves of a
+// bf16 fragment (four requests of one group and of the next) change places in
+// rows 4-7 and 12-15, for the sake of reading eight rows at a time.
 __device__ __forceinline__ int ds_place(int lane)
 {
     return (lane & 48) | ((lane & 15) ^ ((lane >> 4) << 2));
@@ -240,8 +300,6 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_kernel(const DsArgs A)
     if constexpr (TAB)
         for (int i = tid; i < NG * 16 * A.pitch; i += blockDim.x)
             tab[i] = q0 + i / A.pitch < A.b.B ? A.dout[(size_t)q0 * A.pitch + i] : 0.f;
-    wait_vmcnt<0>();
-    stream_barrier();
     // label gradient column cc of request q of the tile
     auto dout = [&](int q, int cc) -> float {
         if constexpr (TAB)
@@ -381,8 +439,10 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_kernel(const DsArgs A)
                         if (g + 1 < NG)
                             y = dp[r][g + 1 < NG ? g + 1 : g];
                         i32x4 *at = A.ds + ((tile0 + r) * A.n_blk + blk) * 2 * WAVE + place;
-                        at[0] = __builtin_bit_cast(i32x4, f32x4{x[0], x[1], y[0], y[1]});
-                        at[WAVE] = __builtin_bit_cast(i32x4, f32x4{x[2], x[3], y[2], y[3]});
+                        const bool turned = col & 4;
+                        const f32x4 u = turned ? y : x, v = turned ? x : y;
+                        at[0] = __builtin_bit_cast(i32x4, f32x4{u[0], u[1], v[0], v[1]});
+                        at[WAVE] = __builtin_bit_cast(i32x4, f32x4{u[2], u[3], v[2], v[3]});
                     }
                 } else {
 #pragma unroll
@@ -433,7 +493,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_kernel(const DsArgs A)
             }
         }
     };
-    scan_slabs<DT, NG, AT_RT, at_ring(DT, AT_RT), true>(A.b, A.nks, qs, s0, s1, lane, side, end);
+    scan_slabs<DT, NG, AT_RT, at_ring(DT, AT_RT), true>(A.b, A.nks, qs, s0, s1, lane, [] {}, side, end);
 
     // ---- the requests' sums, joined over the waves
     float *jn = (float *)smem;   // [n_waves][NG * 16][2]
@@ -460,42 +520,6 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_kernel(const DsArgs A)
         float *at = A.req + ((size_t)ch * A.b.B + q0) * 2 + i;
         *at = A.first ? s : *at + s;
     }
-}
-
-// Fragments of the requests for d_bank: [block of requests][16 columns][64]
-// lanes, lane (column l % 16, requests 4*(l/16) .. of a group; bf16: of two).
-template <int QDT>
-__global__ __launch_bounds__(256) void qpack_kernel(const uint8_t *queries, int B, int d, int n_blk,
-                                                    int n_dt, i32x4 *out)
-{
-    const long i = (long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (long)n_blk * n_dt * WAVE)
-        return;
-    const int lane = (int)(i % WAVE), dt = (int)(i / WAVE % n_dt), blk = (int)(i / WAVE / n_dt);
-    const int colm = dt * 16 + (lane & 15), jg = lane >> 4;
-    i32x4 r = i32x4{0, 0, 0, 0};
-    if (colm < d) {
-        if constexpr (QDT == 1) {
-            const uint16_t *q = (const uint16_t *)queries;
-            uint32_t v[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int b = blk * 32 + (j >> 2) * 16 + 4 * jg + (j & 3);
-                v[j] = b < B ? q[(size_t)b * d + colm] : 0u;
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                r[j] = (int)(v[2 * j] | (v[2 * j + 1] << 16));
-        } else {
-            const int *q = (const int *)queries;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int b = blk * 16 + 4 * jg + j;
-                r[j] = b < B ? q[(size_t)b * d + colm] : 0;
-            }
-        }
-    }
-    out[i] = r;
 }
 
 // Four elements of a gradient, rounded once.
@@ -530,50 +554,112 @@ struct DxArgs {
     uint8_t *d_bank;
     int n_blk, n_dt, n_qt, d;
     long part_rows, row0, nrows;   // rows of this part
+    int n_row_blocks;              // of 256
     float scale;                   // 2 * beta
 };
 
-constexpr int DX_COLS = 8;   // 16-column tiles of a wave
+constexpr int DX_SLOTS = 4, DX_MOST = 16;   // slots of request fragments, most of them in one
 
-// d_bank of a part: 2 beta (ds^T . q - x * sum of ds). A wave has 32 rows x 128
-// columns, D[column 4*(lane/16) + e][row lane % 16].
-template <int DT>
-__global__ __launch_bounds__(256) void dx_kernel(const DxArgs A)
+// d_bank of a part: 2 beta (ds^T . q - x * sum of ds). A workgroup of 8 waves
+// has 256 rows x NC * 16 columns, a wave 32 rows of all the columns (up to 128
+// accumulator registers); the requests' fragments of a block (NC KB) go through
+// LDS, three blocks ahead, and a wave's fragments of ds straight into registers,
+// two ahead. A stage is 4 * NC MFMAs a wave, its LDS reads half of what the LDS
+// gives in that time.
+template <int DT, int NC>
+__global__ __launch_bounds__(512, 1) void dx_kernel(const DxArgs A)
 {
     constexpr int H = DT == AT_BF16 ? 2 : 1;   // values of ds
     constexpr int MDT = DT == AT_F32 ? 0 : 1;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int SLOT = DX_MOST * WAVE;       // 16-byte places
+    __shared__ __align__(16) i32x4 ring[DX_SLOTS * SLOT];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, jg = lane >> 4;
-    const long r0 = ((long)blockIdx.x * 4 + wave) * AT_SLAB;
-    if (r0 >= A.nrows)
+    // (the columns of a block of rows run on one XCD: ds comes from memory once)
+    int ct, rb_;
+    chunk_and_tile(A.n_row_blocks, (A.n_dt + NC - 1) / NC, &rb_, &ct);
+    if (rb_ >= A.n_row_blocks)
         return;
-    const int dt0 = blockIdx.y * DX_COLS;
-    const int place = ds_place(lane);
-    f32x4 acc[AT_RT][DX_COLS];
+    const long r0 = ((long)rb_ * 8 + wave) * AT_SLAB;
+    const bool any = r0 < A.nrows;
+    const int dt0 = ct * NC;
+    const __amdgpu_buffer_rsrc_t rq =
+        make_rsrc(A.qpack, (uint32_t)((size_t)A.n_blk * A.n_dt * WAVE * 16));
+    const __amdgpu_buffer_rsrc_t rs =
+        make_rsrc(A.ds + (any ? (r0 / 16) * A.n_blk * H * WAVE : 0),
+                  any ? (uint32_t)(AT_RT * A.n_blk * H * WAVE * 16) : 0u);
+    const uint32_t place = (uint32_t)ds_place(lane) * 16;
+    auto fetch = [&](int blk) {   // two fragments of block blk by this wave
 #pragma unroll
-    for (int r = 0; r < AT_RT; ++r)
-#pragma unroll
-        for (int k = 0; k < DX_COLS; ++k)
-            acc[r][k] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const i32x4 *ds = A.ds + (r0 / 16) * A.n_blk * H * WAVE + place;
-    for (int blk = 0; blk < A.n_blk; ++blk) {
-        i32x4 s[AT_RT][H];
+        for (int j = 0; j < 2; ++j) {
+            const int f = wave + 8 * j;
+            dma16(rq, ring + (blk % DX_SLOTS) * SLOT + f * WAVE,
+                  blk < A.n_blk && f < NC && dt0 + f < A.n_dt
+                      ? (uint32_t)(((blk * A.n_dt + dt0 + f) * WAVE + lane) * 16)
+                      : OFF_NONE);
+        }
+    };
+    i32x4 s[2][AT_RT][H];
+    auto load_ds = [&](int blk, i32x4(&to)[AT_RT][H]) {
 #pragma unroll
         for (int r = 0; r < AT_RT; ++r)
 #pragma unroll
             for (int h = 0; h < H; ++h)
-                s[r][h] = ds[((size_t)r * A.n_blk + blk) * H * WAVE + h * WAVE];
-        const i32x4 *qp = A.qpack + ((size_t)blk * A.n_dt + dt0) * WAVE + lane;
+                to[r][h] = buffer_load16(
+                    rs, blk < A.n_blk
+                            ? (uint32_t)(((r * A.n_blk + blk) * H + h) * WAVE * 16) + place
+                            : OFF_NONE);
+    };
+    f32x4 acc[AT_RT][NC];
 #pragma unroll
-        for (int k = 0; k < DX_COLS; ++k) {
-            const i32x4 q = qp[(dt0 + k < A.n_dt ? k : 0) * WAVE];
+    for (int r = 0; r < AT_RT; ++r)
 #pragma unroll
-            for (int r = 0; r < AT_RT; ++r)
+        for (int k = 0; k < NC; ++k)
+            acc[r][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    __builtin_amdgcn_sched_barrier(0);
+    fetch(0);
+    fetch(1);
+    load_ds(0, s[0]);
+    fetch(2);
+    load_ds(1, s[1]);
+    for (int b0 = 0; b0 < A.n_blk; b0 += 2) {
+        static_for<0, 2>([&](auto U) {
+            constexpr int u = decltype(U)::value;
+            const int blk = b0 + u;
+            __builtin_amdgcn_sched_barrier(0);
+            // this wave's part of the block and its ds are there once only what
+            // was sent after them is outstanding; after the barrier every wave's
+            // part is, and no wave reads the slot of the block before any more
+            wait_vmcnt<2 + AT_RT * H>();
+            stream_barrier();
+            fetch(blk + 3);
+            __builtin_amdgcn_sched_barrier(0);
+            const i32x4 *slot = ring + (blk % DX_SLOTS) * SLOT + lane;
+            if constexpr (DT == AT_BF16) {   // (halves in their places again)
+                const bool turned = col & 4;
 #pragma unroll
-                for (int h = 0; h < H; ++h)
-                    acc[r][k] = mfma_step<MDT>(q, s[r][h], acc[r][k]);
-        }
+                for (int r = 0; r < AT_RT; ++r)
+#pragma unroll
+                    for (int h = 0; h < H; ++h) {
+                        const i32x4 x = s[u][r][h];
+                        s[u][r][h] = turned ? i32x4{x[2], x[3], x[0], x[1]} : x;
+                    }
+            }
+#pragma unroll
+            for (int k = 0; k < NC; ++k) {
+                const i32x4 q = slot[k * WAVE];
+#pragma unroll
+                for (int r = 0; r < AT_RT; ++r)
+#pragma unroll
+                    for (int h = 0; h < H; ++h)
+                        acc[r][k] = mfma_step<MDT>(q, s[u][r][h], acc[r][k]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            load_ds(blk + 2, s[u]);
+        });
     }
+    wait_vmcnt<0>();   // (no global-to-LDS load in flight when the workgroup ends)
 #pragma unroll
     for (int r = 0; r < AT_RT; ++r) {
         const long lr = r0 + r * 16 + col;
@@ -585,8 +671,8 @@ __global__ __launch_bounds__(256) void dx_kernel(const DxArgs A)
         const size_t row = (size_t)(A.row0 + lr);
         const bool live = !A.mask || A.mask[row] != 0;
 #pragma unroll
-        for (int k = 0; k < DX_COLS; ++k) {
-            const int c0 = (dt0 + k) * 16 + 4 * jg;
+        for (int k = 0; k < NC; ++k) {
+            const int c0 = dealt_column(dt0 + k, 4 * jg);
             if (c0 >= A.d)
                 continue;
             const f32x4 x = load4<DT>(A.rows, row * A.d + c0);
@@ -609,32 +695,57 @@ struct DqArgs {
 };
 
 constexpr int DQ_COLS = 256, DQ_GROUPS = 8;   // columns and request groups of a workgroup
+constexpr int DQ_MASKS = 1024;                // most slabs of a share
+
+template <int DT> struct DqLayout {
+    static constexpr int H = DT == AT_BF16 ? 2 : 1;
+    static constexpr int ESZ = DT == AT_F32 ? 4 : 2;
+    static constexpr int NB = DT == AT_BF16 ? DQ_GROUPS / 2 : DQ_GROUPS;   // blocks of requests
+    static constexpr int ROWB = DQ_COLS * ESZ;               // bytes of a row in LDS
+    static constexpr int XB = AT_SLAB * ROWB;                // of a slab's rows
+    static constexpr int SB = AT_RT * NB * H * WAVE * 16;    // of its ds, [2][NB][H][64]
+    static constexpr int SLOTS = DT == AT_F32 ? 3 : 4;
+    static constexpr size_t BYTES = (size_t)SLOTS * (XB + SB) + DQ_MASKS * 4;
+};
 
 // Partial d_queries of a share of a part: sum over its rows of ds * row. A
-// workgroup of 8 waves has 256 columns x 128 requests, a wave 64 x 64; 32 rows
-// at a time go through LDS, read across (ds_read_b64_tr_b16: four rows of 16
-// columns become a column's four rows per lane) for the product over rows:
-// D[column 4*(lane/16) + e][request lane % 16].
+// workgroup of 8 waves has 256 columns x 128 requests, a wave 64 x 64; slabs of
+// 32 rows go through LDS, SLOTS - 1 ahead (with one ahead a slab's 512 cycles of
+// MFMA waited for memory: 256 x 100,000 x 768 took 164 us for less than half), and are read
+// across (ds_read_b64_tr_b16: four rows of 16 columns become a column's four
+// rows per lane) for the product over rows: D[column 4*(lane/16) + e][request
+// lane % 16]. Masked rows hold anything and are not fetched: zeros.
 template <int DT>
 __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
 {
-    constexpr int H = DT == AT_BF16 ? 2 : 1;
-    constexpr int ESZ = DT == AT_F32 ? 4 : 2;
-    constexpr int ROWB = DQ_COLS * ESZ;               // bytes of a row in LDS
-    constexpr int XB = AT_SLAB * ROWB;                // a slab's rows
-    // ds of a slab: bf16 [2 row tiles][4 blocks][2][64], fp32 [2][8][64] of 16 bytes
-    constexpr int NB = DT == AT_BF16 ? DQ_GROUPS / 2 : DQ_GROUPS;
-    constexpr int SB = AT_RT * NB * H * WAVE * 16;
+    using L = DqLayout<DT>;
+    constexpr int H = L::H, ESZ = L::ESZ, ROWB = L::ROWB, XB = L::XB, SB = L::SB, NB = L::NB;
+    constexpr int SLOTS = L::SLOTS;
     extern __shared__ __align__(16) uint8_t smem[];
+    uint32_t *keep = (uint32_t *)(smem + SLOTS * (XB + SB));   // [slab of the share] a bit a row
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, jg = lane >> 4;
     const int wd = wave & 3, wq = wave >> 2;   // 64 columns, 4 groups of this wave
-    const int c0 = blockIdx.y * DQ_COLS, b0 = blockIdx.z * NB;
-    const long z0 = (long)blockIdx.x * A.slabs / A.n_chunks,
-               z1 = (long)(blockIdx.x + 1) * A.slabs / A.n_chunks;
+    // (a share's tiles run on one XCD: its rows and its ds come from memory once)
+    const int n_ct = (A.d + DQ_COLS - 1) / DQ_COLS, n_bt = (A.n_blk + NB - 1) / NB;
+    int ch, t;
+    chunk_and_tile(A.n_chunks, n_ct * n_bt, &ch, &t);
+    if (ch >= A.n_chunks)
+        return;
+    const int c0 = t % n_ct * DQ_COLS, b0 = t / n_ct * NB;
+    const long z0 = (long)ch * A.slabs / A.n_chunks, z1 = (long)(ch + 1) * A.slabs / A.n_chunks;
     const uint32_t rowb = (uint32_t)A.d * ESZ;
 
+    if (A.mask) {
+        for (long z = z0 + wave; z < z1; z += 8) {
+            const long row = z * AT_SLAB + (lane & 31);
+            const uint64_t b = ballot(row < A.nrows && A.mask[A.row0 + row] != 0);
+            if (lane == 0)
+                keep[z - z0] = (uint32_t)b;
+        }
+        __syncthreads();
+    }
     f32x4 acc[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -642,27 +753,28 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
         for (int g = 0; g < 4; ++g)
             acc[i][g] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    // slab z into buffer (z - z0) & 1
     constexpr int XL = XB / 1024, SL = SB / 1024;   // loads of 64 x 16 bytes
     auto issue = [&](long z) {
-        uint8_t *buf = smem + ((z - z0) & 1) * (XB + SB);
+        uint8_t *buf = smem + ((z - z0) % SLOTS) * (XB + SB);
         const long r0 = z * AT_SLAB;
-        const int rows = (int)max(0L, min((long)AT_SLAB, A.nrows - r0));
-        const __amdgpu_buffer_rsrc_t rx = make_rsrc(A.rows + (size_t)(A.row0 + r0) * rowb,
-                                                    z < z1 ? (uint32_t)rows * rowb : 0u);
+        const bool in = z < z1;
+        const int rows = in ? (int)min((long)AT_SLAB, A.nrows - r0) : 0;
+        const __amdgpu_buffer_rsrc_t rx = make_rsrc(A.rows + (size_t)(A.row0 + (in ? r0 : 0)) * rowb,
+                                                    (uint32_t)rows * rowb);
+        const uint32_t live = A.mask && in ? keep[z - z0] : ~0u;
 #pragma unroll
         for (int j = 0; j < XL / 8; ++j) {
             const int f = wave * (XL / 8) + j;
             const int pos = f * 64 + lane;              // 16-byte places, row by row
             const int row = pos / (ROWB / 16), at = pos % (ROWB / 16);
-            const int swz = DT == AT_BF16 ? (row & 3) * 2 : ((row >> 2) & 3) * 4;
+            const int swz = DT == AT_BF16 ? (row & 7) * 2 : ((row >> 2) & 3) * 4;
             const uint32_t byte = (uint32_t)c0 * ESZ + (uint32_t)(at ^ swz) * 16;
             dma16(rx, (i32x4 *)(buf + f * 1024),
-                  byte < rowb ? (uint32_t)row * rowb + byte : OFF_NONE);
+                  byte < rowb && (live >> row & 1) ? (uint32_t)row * rowb + byte : OFF_NONE);
         }
         const __amdgpu_buffer_rsrc_t rs =
-            make_rsrc(A.ds + (size_t)z * AT_RT * A.n_blk * H * WAVE,
-                      z < z1 ? (uint32_t)(AT_RT * A.n_blk * H * WAVE * 16) : 0u);
+            make_rsrc(A.ds + (size_t)(in ? z : 0) * AT_RT * A.n_blk * H * WAVE,
+                      in ? (uint32_t)(AT_RT * A.n_blk * H * WAVE * 16) : 0u);
 #pragma unroll
         for (int j = 0; j < SL / 8; ++j) {
             const int f = wave * (SL / 8) + j;
@@ -674,43 +786,39 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
         }
     };
     constexpr int LOADS = XL / 8 + SL / 8;
-    issue(z0);
+    for (int k = 0; k < SLOTS - 1; ++k)
+        issue(z0 + k);
     for (long z = z0; z < z1; ++z) {
-        issue(z + 1);
-        wait_vmcnt<LOADS>();
+        __builtin_amdgcn_sched_barrier(0);
+        // slab z has landed for every wave, and slab z - 1 is read
+        wait_vmcnt<(SLOTS - 2) * LOADS>();
         stream_barrier();
-        const uint8_t *xb = smem + ((z - z0) & 1) * (XB + SB), *sb = xb + XB;
+        issue(z + SLOTS - 1);
+        __builtin_amdgcn_sched_barrier(0);
+        const uint8_t *xb = smem + ((z - z0) % SLOTS) * (XB + SB), *sb = xb + XB;
         if constexpr (DT == AT_BF16) {
             typedef short s16x4 __attribute__((ext_vector_type(4)));
+            typedef int i32x2 __attribute__((ext_vector_type(2)));
             typedef __attribute__((address_space(3))) s16x4 *lds4;
-            // rows that are masked hold anything: 0 in their places
-            uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
-            if (A.mask) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const long row = z * AT_SLAB + (j >> 2) * 16 + 4 * jg + (j & 3);
-                    const bool ok = row < A.nrows && A.mask[A.row0 + row] != 0;
-                    if (!ok)
-                        keep[j >> 1] &= (j & 1) ? 0x0000ffffu : 0xffff0000u;
-                }
-            }
+            auto across = [](const uint8_t *p) {
+                return __builtin_bit_cast(i32x2,
+                                          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)p));
+            };
             i32x4 a[4];
             const int ti = lane & 15;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     const int row = r * 16 + 4 * jg + (ti >> 2);
                     const int el = wd * 64 + i * 16 + 4 * (ti & 3);
-                    const uint8_t *p =
-                        xb + row * ROWB + ((el >> 3) ^ ((row & 3) * 2)) * 16 + (el & 7) * 2;
-                    const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)p);
-                    typedef int i32x2 __attribute__((ext_vector_type(2)));
-                    const i32x2 w = __builtin_bit_cast(i32x2, v);
-                    a[i][2 * r] = (int)((uint32_t)w[0] & keep[2 * r]);
-                    a[i][2 * r + 1] = (int)((uint32_t)w[1] & keep[2 * r + 1]);
+                    const i32x2 w = across(xb + row * ROWB +
+                                           ((el >> 3) ^ ((row & 7) * 2)) * 16 + (el & 7) * 2);
+                    a[i][2 * r] = w[0];
+                    a[i][2 * r + 1] = w[1];
                 }
-            }
+            // the lane that wrote the four values this one reads across
+            const int src = ds_place((ti & 3) * 16 + 4 * jg + (ti >> 2)) * 16;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 // group wq*4 + g: half g & 1 of block wq*2 + g/2
@@ -719,13 +827,9 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
                     i32x4 s;
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const int src = (ti & 3) * 16 + 4 * jg + (ti >> 2);   // the lane that wrote it
-                        const uint8_t *p = sb +
-                                           (size_t)((r * NB + wq * 2 + (g >> 1)) * 2 + h) * 1024 +
-                                           ds_place(src) * 16 + (g & 1) * 8;
-                        const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)p);
-                        typedef int i32x2 __attribute__((ext_vector_type(2)));
-                        const i32x2 w = __builtin_bit_cast(i32x2, v);
+                        const i32x2 w =
+                            across(sb + ((r * NB + wq * 2 + (g >> 1)) * 2 + h) * 1024 + src +
+                                   ((g ^ jg) & 1) * 8);
                         s[2 * r] = w[0];
                         s[2 * r + 1] = w[1];
                     }
@@ -740,23 +844,17 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int row = r * 16 + 4 * jg + e;
-                    bool ok = true;
-                    if (A.mask) {
-                        const long at = z * AT_SLAB + row;
-                        ok = at < A.nrows && A.mask[A.row0 + at] != 0;
-                    }
                     float x[4], s[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int el = wd * 64 + i * 16 + col;
-                        const float y = *(const float *)(xb + row * ROWB +
-                                                         ((el >> 2) ^ (jg * 4)) * 16 + (el & 3) * 4);
-                        x[i] = ok ? y : 0.f;
+                        x[i] = *(const float *)(xb + row * ROWB + ((el >> 2) ^ (jg * 4)) * 16 +
+                                                (el & 3) * 4);
                     }
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
                         const int src = (col >> 2) * 16 + 4 * jg + e;
-                        s[g] = *(const float *)(sb + (size_t)(r * NB + wq * 4 + g) * 1024 +
+                        s[g] = *(const float *)(sb + (r * NB + wq * 4 + g) * 1024 +
                                                 ds_place(src) * 16 + (col & 3) * 4);
                     }
 #pragma unroll
@@ -768,7 +866,6 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
                 }
             }
         }
-        stream_barrier();   // (the slab after next comes into this buffer)
     }
     wait_vmcnt<0>();
 #pragma unroll
@@ -778,13 +875,14 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
             const int cc = c0 + wd * 64 + i * 16 + 4 * jg;
             const int b = (DT == AT_BF16 ? b0 * 32 : b0 * 16) + (wq * 4 + g) * 16 + col;
             if (cc < A.d && b < A.B) {
-                f32x4 *at = (f32x4 *)(A.part + ((size_t)blockIdx.x * A.B + b) * A.d + cc);
+                f32x4 *at = (f32x4 *)(A.part + ((size_t)ch * A.B + b) * A.d + cc);
                 *at = A.first ? acc[i][g] : *at + acc[i][g];
             }
         }
 }
 
-// d_queries and d_beta: the shares' sums, 2 beta (sum - q * sum of ds).
+// d_queries and d_beta: the shares' sums, 2 beta (sum - q * sum of ds). One
+// workgroup per request and 256 columns, a wave every fourth share.
 template <int DT>
 __global__ __launch_bounds__(256) void dq_join_kernel(const float *part, int n_part,
                                                       const float *req, int n_req,
@@ -792,47 +890,57 @@ __global__ __launch_bounds__(256) void dq_join_kernel(const float *part, int n_p
                                                       float scale, uint8_t *d_queries,
                                                       float *d_beta)
 {
-    __shared__ float red[2][256];
-    const int b = blockIdx.x, tid = threadIdx.x;
+    __shared__ float red[2][4];
+    __shared__ f32x4 sums[3][WAVE];
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int c0 = blockIdx.y * 256 + lane * 4;
+    const bool in = d_queries && c0 < d;
+    f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (in) {
+        const float *at = part + (size_t)b * d + c0;
+        const size_t step = (size_t)B * d;
+#pragma unroll 8
+        for (int k = wave; k < n_part; k += 4)
+            v += *(const f32x4 *)(at + k * step);
+    }
     float s0 = 0.f, s1 = 0.f;
     for (int k = tid; k < n_req; k += 256) {
         const float *at = req + ((size_t)k * B + b) * 2;
         s0 += at[0];
         s1 += at[1];
     }
-    red[0][tid] = s0;
-    red[1][tid] = s1;
+    s0 = wave_sum(s0);
+    s1 = wave_sum(s1);
+    if (lane == 0) {
+        red[0][wave] = s0;
+        red[1][wave] = s1;
+    }
+    if (wave > 0)
+        sums[wave - 1][lane] = v;
     __syncthreads();
-    for (int k = 128; k > 0; k >>= 1) {
-        if (tid < k) {
-            red[0][tid] += red[0][tid + k];
-            red[1][tid] += red[1][tid + k];
-        }
-        __syncthreads();
-    }
-    const float sum = red[0][0];
-    if (tid == 0 && d_beta)
-        d_beta[b] = red[1][0];
-    if (!d_queries)
+    if (tid == 0 && blockIdx.y == 0 && d_beta)
+        d_beta[b] = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+    if (wave > 0 || !in)
         return;
-    for (int c0 = tid * 4; c0 < d; c0 += 1024) {
-        f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < n_part; ++k)
-            v += *(const f32x4 *)(part + ((size_t)k * B + b) * d + c0);
-        const f32x4 q = load4<DT>(queries, (size_t)b * d + c0);
+    const float sum = (red[0][0] + red[0][1]) + (red[0][2] + red[0][3]);
+    for (int w = 0; w < 3; ++w)
+        v += sums[w][lane];
+    const f32x4 q = load4<DT>(queries, (size_t)b * d + c0);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            v[e] = scale * (v[e] - q[e] * sum);
-        store4<DT>(d_queries, (size_t)b * d + c0, v);
-    }
+    for (int e = 0; e < 4; ++e)
+        v[e] = scale * (v[e] - q[e] * sum);
+    store4<DT>(d_queries, (size_t)b * d + c0, v);
 }
 
-// The request tiles' label gradients, added in order.
-__global__ __launch_bounds__(256) void label_join_kernel(const float *part, int n_qt, size_t n,
-                                                         float *out)
+// The request tiles' label gradients, added in order (grid.y: one or both kinds).
+__global__ __launch_bounds__(256) void label_join_kernel(const float *part0, float *out0,
+                                                         const float *part1, float *out1, int n_qt,
+                                                         size_t n)
 {
     const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n)
+    const float *part = blockIdx.y ? part1 : part0;
+    float *out = blockIdx.y ? out1 : out0;
+    if (i >= n || !out)
         return;
     float s = 0.f;
     for (int t = 0; t < n_qt; ++t)
@@ -909,13 +1017,20 @@ void shares(int slabs, int slab, int dtype, int d, int n_qt, int n_cu, int *n_ch
 }
 
 template <int QDT>
-hipError_t run_side(const AttendBank &b, int M, const float *lse, const GradArgs *g, float *dout,
-                    int pitch, Side *side, hipStream_t s)
+hipError_t run_prep(const PrepArgs &a, hipStream_t s)
 {
-    hipLaunchKernelGGL(side_kernel<QDT>, dim3((b.B + 3) / 4), dim3(256), 0, s, b.queries, b.B, b.d,
-                       M, lse, g ? g->q_hat : nullptr, g ? g->l_hat : nullptr,
-                       g ? g->dq_hat : nullptr, g ? g->dl_hat : nullptr, g ? g->dlse : nullptr,
-                       dout, pitch, side);
+    const int side_blocks = (a.B + 3) / 4;
+    const long frags = a.qpack ? (long)a.n_blk * a.n_dt * WAVE : 0;
+    hipLaunchKernelGGL(prep_kernel<QDT>, dim3((unsigned)(side_blocks + (frags + 255) / 256)),
+                       dim3(256), 0, s, a, side_blocks);
+    return hipGetLastError();
+}
+
+template <int DT, int NC>
+hipError_t dx_one(const DxArgs &x, hipStream_t s)
+{
+    hipLaunchKernelGGL((dx_kernel<DT, NC>), dim3(x.n_row_blocks * ((x.n_dt + NC - 1) / NC)),
+                       dim3(512), 0, s, x);
     return hipGetLastError();
 }
 
@@ -924,21 +1039,16 @@ hipError_t run_grad(const GradPlan &p, const AttendBank &b, const GradArgs &g, u
                     hipStream_t s)
 {
     constexpr int QDT = DT == AT_F32 ? 0 : 1;
-    constexpr int H = DT == AT_BF16 ? 2 : 1;
     Side *side = (Side *)(wb + p.off_side);
     float *dout = (float *)(wb + p.off_dout);
     i32x4 *qpack = (i32x4 *)(wb + p.off_qpack);
-    hipError_t e = run_side<QDT>(b, g.M, g.lse, &g, dout, p.pitch, side, s);
+    const int n_dt = p.n_dt;
+    hipError_t e = run_prep<QDT>({b.queries, b.B, b.d, g.M, p.pitch, g.lse, g.q_hat, g.l_hat,
+                                  g.dq_hat, g.dl_hat, g.dlse, dout, side, p.n_blk, n_dt,
+                                  g.d_bank ? qpack : nullptr},
+                                 s);
     if (e != hipSuccess)
         return e;
-    const int n_dt = (b.d + 15) / 16;
-    if (g.d_bank) {
-        const long n = (long)p.n_blk * n_dt * WAVE;
-        hipLaunchKernelGGL(qpack_kernel<QDT>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s,
-                           b.queries, b.B, b.d, p.n_blk, n_dt, qpack);
-        if ((e = hipGetLastError()) != hipSuccess)
-            return e;
-    }
     DsArgs a;
     a.b = b;
     a.qual = g.qual;
@@ -973,44 +1083,41 @@ hipError_t run_grad(const GradPlan &p, const AttendBank &b, const GradArgs &g, u
         if (g.d_queries) {
             DqArgs q{a.ds, b.rows, b.mask, b.B, b.d, p.n_blk, p.q_chunks, row0, nrows, slabs, dq,
                      z0 == 0};
-            constexpr int NB = DT == AT_BF16 ? DQ_GROUPS / 2 : DQ_GROUPS;
-            const size_t lds = 2 * (size_t)(AT_SLAB * DQ_COLS * (DT == AT_F32 ? 4 : 2) +
-                                            AT_RT * NB * H * WAVE * 16);
-            if ((e = allow_lds(dq_kernel<DT>, lds)) != hipSuccess)
+            using L = DqLayout<DT>;
+            if ((e = allow_lds(dq_kernel<DT>, L::BYTES)) != hipSuccess)
                 return e;
             hipLaunchKernelGGL(dq_kernel<DT>,
-                               dim3(p.q_chunks, (b.d + DQ_COLS - 1) / DQ_COLS,
-                                    (p.n_blk + NB - 1) / NB),
-                               dim3(512), lds, s, q);
+                               dim3(p.q_chunks * ((b.d + DQ_COLS - 1) / DQ_COLS) *
+                                    ((p.n_blk + L::NB - 1) / L::NB)),
+                               dim3(512), L::BYTES, s, q);
             if ((e = hipGetLastError()) != hipSuccess)
                 return e;
         }
         if (g.d_bank) {
             DxArgs x{a.ds, qpack, a.rowsum, b.rows, b.mask, (uint8_t *)g.d_bank, p.n_blk, n_dt,
-                     p.n_qt, b.d, a.part_rows, row0, nrows, scale};
-            hipLaunchKernelGGL(dx_kernel<DT>,
-                               dim3((unsigned)((nrows + 4 * AT_SLAB - 1) / (4 * AT_SLAB)),
-                                    (n_dt + DX_COLS - 1) / DX_COLS),
-                               dim3(256), 0, s, x);
-            if ((e = hipGetLastError()) != hipSuccess)
+                     p.n_qt, b.d, a.part_rows, row0, nrows,
+                     (int)((nrows + 8 * AT_SLAB - 1) / (8 * AT_SLAB)), scale};
+            // as many columns to a workgroup as leave few of the last one's idle
+            const int per = (n_dt + (n_dt + DX_MOST - 1) / DX_MOST - 1) /
+                            ((n_dt + DX_MOST - 1) / DX_MOST);
+            e = per > 12 ? dx_one<DT, 16>(x, s) : per > 8 ? dx_one<DT, 12>(x, s) : dx_one<DT, 8>(x, s);
+            if (e != hipSuccess)
                 return e;
         }
     }
     if (g.d_queries || g.d_beta) {
-        hipLaunchKernelGGL(dq_join_kernel<DT>, dim3(b.B), dim3(256), 0, s, dq, p.q_chunks, a.req,
+        hipLaunchKernelGGL(dq_join_kernel<DT>,
+                           dim3(b.B, g.d_queries ? (b.d + 255) / 256 : 1), dim3(256), 0, s, dq, p.q_chunks, a.req,
                            p.n_chunks, b.queries, b.B, b.d, scale, (uint8_t *)g.d_queries,
                            g.d_beta);
         if ((e = hipGetLastError()) != hipSuccess)
             return e;
     }
     if (p.n_qt > 1) {
-        const unsigned blocks = (unsigned)((n_lab + 255) / 256);
-        if (g.d_qual)
-            hipLaunchKernelGGL(label_join_kernel, dim3(blocks), dim3(256), 0, s, a.d_qual, p.n_qt,
-                               n_lab, g.d_qual);
-        if (g.d_len)
-            hipLaunchKernelGGL(label_join_kernel, dim3(blocks), dim3(256), 0, s, a.d_len, p.n_qt,
-                               n_lab, g.d_len);
+        if (g.d_qual || g.d_len)
+            hipLaunchKernelGGL(label_join_kernel, dim3((unsigned)((n_lab + 255) / 256), 2),
+                               dim3(256), 0, s, a.d_qual, g.d_qual, a.d_len, g.d_len, p.n_qt,
+                               n_lab);
         e = hipGetLastError();
     }
     return e;
@@ -1045,8 +1152,13 @@ hipError_t launch_usage(const UsagePlan &p, const AttendBank &b, const float *ls
                         float *usage, void *ws, hipStream_t s)
 {
     Side *side = (Side *)((uint8_t *)ws + p.off_side);
-    hipError_t e = p.dtype == AT_F32 ? run_side<0>(b, 0, lse, nullptr, nullptr, 0, side, s)
-                                     : run_side<1>(b, 0, lse, nullptr, nullptr, 0, side, s);
+    PrepArgs pa{};
+    pa.queries = b.queries;
+    pa.B = b.B;
+    pa.d = b.d;
+    pa.lse = lse;
+    pa.side = side;
+    hipError_t e = p.dtype == AT_F32 ? run_prep<0>(pa, s) : run_prep<1>(pa, s);
     if (e != hipSuccess)
         return e;
     UsageArgs a;
@@ -1120,11 +1232,17 @@ bool plan_grad(int B, int N, int d, int dtype, int M, int n_cu, GradPlan *p)
                        ((B + DQ_GROUPS * 16 - 1) / (DQ_GROUPS * 16));
     long qc = n_cu / tiles;
     qc = qc < 1 ? 1 : qc;
+    // (a share's masks are kept in LDS)
+    const long least = (part + DQ_MASKS - 1) / DQ_MASKS;
+    qc = qc < least ? least : qc;
     p->q_chunks = (int)(qc > part ? part : qc);
     const size_t lds = (group + (p->tab ? tab : 0)) * ng;
     const size_t join = (size_t)p->waves * ng * 16 * 2 * 4;
     p->lds_bytes = lds > join ? lds : join;
-    const int n_dt = (d + 15) / 16;
+    const int n_dt = (d + 31) / 32 * 2;
+    p->n_dt = n_dt;
+    if ((size_t)p->n_blk * n_dt * WAVE * 16 >= (size_t)1 << 31)   // (32-bit offsets)
+        return false;
     size_t o = 0;
     p->off_side = o;
     o += up256((size_t)B * sizeof(Side));

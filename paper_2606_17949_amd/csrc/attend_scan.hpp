@@ -72,7 +72,8 @@ __device__ __forceinline__ i32x4 widen4(uint32_t codes, float scale)
 // One wave's pass over slabs [s0, s1) (of 16 * RT rows) of the bank against the
 // request tile in LDS. Bank rows come from HBM straight into MFMA operand
 // registers, R k-steps (a block) ahead across slab ends, and no wave waits for
-// another. side(slab) sends for what end(slab, acc) reads beside the products.
+// another once the request tile, sent for before the call, has landed; ready()
+// is called then, in every wave. side(slab) sends for what end(slab, acc) reads beside the products.
 // A slab's first block stands apart from the others: there the compiler knows
 // that side's loads came after the block's own, so that waiting for the block
 // does not wait for them. (In one loop over all blocks every slab emptied the
@@ -81,9 +82,10 @@ __device__ __forceinline__ i32x4 widen4(uint32_t codes, float scale)
 // BANK_COLS false: acc[r][g][e] is <q, x> of row 16*r + 4*(lane/16) + e and
 // request 16*g + lane%16; true: of row 16*r + lane%16 and request
 // 16*g + 4*(lane/16) + e.
-template <int DT, int NG, int RT, int R, bool BANK_COLS, typename Side, typename End>
+template <int DT, int NG, int RT, int R, bool BANK_COLS, typename Ready, typename Side, typename End>
 __device__ __forceinline__ void scan_slabs(const AttendBank &A, int nks, const i32x4 *qs, long s0,
-                                           long s1, int lane, Side &&side, End &&end)
+                                           long s1, int lane, Ready &&ready, Side &&side,
+                                           End &&end)
 {
     using E = AtElem<DT>;
     constexpr int MDT = DT == AT_F32 ? 0 : 1;
@@ -91,8 +93,12 @@ __device__ __forceinline__ void scan_slabs(const AttendBank &A, int nks, const i
     const int col = lane & 15, jg = lane >> 4;
     const uint32_t rowb = at_row_bytes(DT, A.d);
     const int n_slabs = (int)(s1 - s0);
-    if (n_slabs <= 0)
+    if (n_slabs <= 0) {   // (every wave meets at the barrier)
+        wait_vmcnt<0>();
+        stream_barrier();
+        ready();
         return;
+    }
     const long row0 = s0 * SLAB;
     const int nrows = (int)min((long)n_slabs * SLAB, A.N - row0);
     const __amdgpu_buffer_rsrc_t rbk =
@@ -127,8 +133,16 @@ __device__ __forceinline__ void scan_slabs(const AttendBank &A, int nks, const i
             ++ls;
         }
     };
+    __builtin_amdgcn_sched_barrier(0);
     static_for<0, R>([&](auto U) { issue(U); });
     advance();
+    // the request tile has landed once at most the loads after it are
+    // outstanding, and after the barrier in every wave
+    __builtin_amdgcn_sched_barrier(0);
+    wait_vmcnt<R * RT * (DT == AT_Q4 ? 2 : 1)>();
+    stream_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    ready();
 
     f32x4 acc[RT][NG];
     // the products of block b, and the loads of the block after it

@@ -106,206 +106,296 @@ __global__ __launch_bounds__(256) void write_rows_kernel(const RowsArgs A)
 // ---- the n least of N, by three histograms of the ordered bits of the keys
 // (11, 11 and 10 of them), which leave the n-th least key T and how many of
 // those equal to it are taken; then every block counts its rows below T and at
-// T, and writes its own behind those of the blocks before it.
-constexpr int EV_BINS = 2048, EV_THREADS = 256, EV_ROWS = 8192;
+// T, and writes its own behind those of the blocks before it. What bounds it is
+// latency: five passes over 4 bytes a row, each a launch. Usage falls into few
+// of the first histogram's bins (of one exponent and two bits of mantissa), so
+// blocks add to one of EV_COPIES histograms, and the n-th key's bin is found by
+// every block of the next pass for itself (found by the last block of a pass to
+// arrive, with a counter and fences between, a pass over 4,000,000 rows took 42
+// us).
+constexpr int EV_BINS = 2048, EV_THREADS = 1024, EV_COPIES = 8;
+constexpr int EV_TILE = EV_THREADS * 4;   // rows a block takes at a time, four a thread
+constexpr int EV_BLOCKS = 256;            // most blocks
 
+// Where the search stands behind each histogram: the bits of T found so far,
+// the rows to take among those with these bits, and whether there are fewer
+// rows than asked for and all are taken.
 struct EvictState {
-    uint32_t ticket[3];
-    uint32_t prefix;   // the bits of T found so far
-    uint32_t remain;   // rows to take among those with these bits
-    uint32_t all;      // fewer rows than asked for: every one is taken
+    uint32_t prefix, remain, all, none;
 };
 
 __device__ __forceinline__ uint32_t usage_key(float u) { return f2key(u + 0.f); }   // -0 is 0
 
-__global__ __launch_bounds__(EV_THREADS) void evict_clear_kernel(uint32_t *hist, EvictState *st,
-                                                                 uint32_t n)
+// Rows i .. i+3: their keys, and which of them may go (none past the end).
+struct Four {
+    uint32_t key[4];
+    bool in[4];
+};
+
+__device__ __forceinline__ Four load_four(const float *usage, const uint8_t *may_go, long i, int N)
 {
-    const int i = blockIdx.x * EV_THREADS + threadIdx.x;
-    if (i < 3 * EV_BINS)
-        hist[i] = 0;
-    if (i == 0) {
-        st->ticket[0] = st->ticket[1] = st->ticket[2] = 0;
-        st->prefix = 0;
-        st->remain = n;
-        st->all = 0;
+    typedef uint32_t u32_any __attribute__((aligned(1)));
+    Four f;
+    if (i + 4 <= N) {
+        const f32x4 u = *(const f32x4_any *)(usage + i);
+        const uint32_t go = may_go ? *(const u32_any *)(may_go + i) : ~0u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            f.key[e] = usage_key(u[e]);
+            f.in[e] = (go >> (8 * e) & 0xffu) != 0;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool at = i + e < N;
+            f.key[e] = at ? usage_key(usage[i + e]) : 0u;
+            f.in[e] = at && (!may_go || may_go[i + e] != 0);
+        }
+    }
+    return f;
+}
+
+__global__ __launch_bounds__(EV_THREADS) void evict_clear_kernel(uint32_t *hist)
+{
+    hist[blockIdx.x * EV_THREADS + threadIdx.x] = 0;
+}
+
+constexpr int ev_bits(int level) { return level == 2 ? 10 : 11; }
+constexpr int ev_shift(int level) { return level == 0 ? 21 : level == 1 ? 10 : 0; }
+
+// The state behind histogram L, from the one before it (L 0: n rows to take).
+// Every thread of the block gets it.
+template <int L>
+__device__ __forceinline__ EvictState evict_pick(const uint32_t *hist_all, EvictState st)
+{
+    constexpr int PER = EV_BINS / EV_THREADS, NW = EV_THREADS / WAVE;
+    static_assert(PER == 2, "the loads below");
+    __shared__ uint32_t sums[NW];
+    __shared__ EvictState found;
+    if (L > 0 && st.all)
+        return st;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    const u32x2 *hist = (const u32x2 *)(hist_all + L * EV_COPIES * EV_BINS);
+    u32x2 own = u32x2{0, 0};
+#pragma unroll
+    for (int k = 0; k < EV_COPIES; ++k)
+        own += hist[k * (EV_BINS / 2) + tid];
+    // rows in the bins of the threads before
+    const uint32_t total = own[0] + own[1];
+    uint32_t upto = total;
+    for (int k = 1; k < WAVE; k <<= 1) {
+        const uint32_t x = (uint32_t)__shfl_up((int)upto, k);
+        upto += lane >= k ? x : 0;
+    }
+    __syncthreads();   // (of an earlier call: read)
+    if (lane == WAVE - 1)
+        sums[wave] = upto;
+    __syncthreads();
+    uint32_t before = upto - total, rows_in = 0;
+    for (int w = 0; w < NW; ++w) {
+        before += w < wave ? sums[w] : 0;
+        rows_in += sums[w];
+    }
+    if (rows_in < st.remain)   // (the first histogram only)
+        return EvictState{0, 0, 1, 0};
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        if (before < st.remain && st.remain <= before + own[j])
+            found = EvictState{(st.prefix << ev_bits(L)) | (uint32_t)(tid * PER + j),
+                               st.remain - before, 0, 0};
+        before += own[j];
+    }
+    __syncthreads();
+    return found;
+}
+
+// Histogram L, of the keys that share the bits found so far. states[L - 1] is
+// found and left for the passes behind the next one.
+template <int L>
+__global__ __launch_bounds__(EV_THREADS) void evict_hist_kernel(const float *usage,
+                                                                const uint8_t *may_go, int N, int n,
+                                                                int rows, uint32_t *hist_all,
+                                                                EvictState *states)
+{
+    constexpr int SHIFT = ev_shift(L), BITS = ev_bits(L);
+    constexpr uint32_t MASK = (1u << BITS) - 1;
+    __shared__ uint32_t bins[EV_BINS];
+    const int tid = threadIdx.x;
+    for (int i = tid; i < EV_BINS; i += EV_THREADS)
+        bins[i] = 0;
+    EvictState st{0, (uint32_t)n, 0, 0};
+    if constexpr (L > 0) {
+        if constexpr (L > 1)
+            st = states[L - 2];
+        st = evict_pick<L - 1>(hist_all, st);
+        if (blockIdx.x == 0 && tid == 0)
+            states[L - 1] = st;
+        if (st.all)
+            return;
+    }
+    __syncthreads();
+    const long r0 = (long)blockIdx.x * rows;
+#pragma unroll 4
+    for (int z = 0; z < rows; z += EV_TILE) {
+        const Four f = load_four(usage, may_go, r0 + z + tid * 4, N);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (f.in[e] && (L == 0 || (f.key[e] >> (SHIFT + BITS)) == st.prefix))
+                atomicAdd(&bins[(f.key[e] >> SHIFT) & MASK], 1u);
+    }
+    __syncthreads();
+    uint32_t *mine = hist_all + (L * EV_COPIES + blockIdx.x % EV_COPIES) * EV_BINS;
+    for (int i = tid; i < EV_BINS; i += EV_THREADS)
+        if (bins[i])
+            atomicAdd(&mine[i], bins[i]);
+}
+
+// A block's rows below T and at T.
+__device__ __forceinline__ void below_and_at(const Four &f, uint32_t T, bool all, bool (&lt)[4],
+                                             bool (&eq)[4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        lt[e] = f.in[e] && (all || f.key[e] < T);
+        eq[e] = f.in[e] && !all && f.key[e] == T;
     }
 }
 
-template <int L>
-__global__ __launch_bounds__(EV_THREADS) void evict_hist_kernel(const float *usage,
-                                                                const uint8_t *may_go, int N,
-                                                                uint32_t *hist_all, EvictState *st)
+// Both sums over the block, for every thread.
+__device__ __forceinline__ void block_sums(uint32_t &x, uint32_t &y,
+                                           uint32_t (&red)[2][EV_THREADS / WAVE])
 {
-    constexpr int SHIFT = L == 0 ? 21 : L == 1 ? 10 : 0;
-    constexpr int BITS = L == 2 ? 10 : 11;
-    constexpr uint32_t MASK = (1u << BITS) - 1;
-    __shared__ uint32_t bins[EV_BINS];
-    __shared__ uint32_t sums[EV_THREADS];
-    __shared__ bool last;
-    const int tid = threadIdx.x;
-    uint32_t *hist = hist_all + L * EV_BINS;
-    if (L > 0 && st->all)
-        return;
-    for (int i = tid; i < EV_BINS; i += EV_THREADS)
-        bins[i] = 0;
+    auto add = [](uint32_t a, uint32_t b) { return a + b; };
+    x = wave_reduce(x, add);
+    y = wave_reduce(y, add);
+    const int wave = threadIdx.x >> 6;
     __syncthreads();
-    const uint32_t prefix = L > 0 ? st->prefix : 0;
-    for (long i = (long)blockIdx.x * EV_THREADS + tid; i < N; i += (long)gridDim.x * EV_THREADS) {
-        const uint32_t key = usage_key(usage[i]);
-        const bool in = (!may_go || may_go[i] != 0) &&
-                        (L == 0 || (key >> (SHIFT + BITS)) == prefix);
-        if (in)
-            atomicAdd(&bins[(key >> SHIFT) & MASK], 1u);
+    if ((threadIdx.x & 63) == 0) {
+        red[0][wave] = x;
+        red[1][wave] = y;
     }
     __syncthreads();
-    for (int i = tid; i < EV_BINS; i += EV_THREADS)
-        if (bins[i])
-            atomicAdd(&hist[i], bins[i]);
-    // the last block to get here finds the bin
-    __threadfence();
-    __syncthreads();
-    if (tid == 0)
-        last = atomicAdd(&st->ticket[L], 1u) == gridDim.x - 1;
-    __syncthreads();
-    if (!last)
-        return;
-    __threadfence();
-    constexpr int PER = EV_BINS / EV_THREADS;
-    uint32_t own[PER], total = 0;
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-        own[j] = __hip_atomic_load(&hist[tid * PER + j], __ATOMIC_RELAXED,
-                                   __HIP_MEMORY_SCOPE_AGENT);
-        total += own[j];
-    }
-    sums[tid] = total;
-    __syncthreads();
-    for (int k = 1; k < EV_THREADS; k <<= 1) {
-        const uint32_t x = tid >= k ? sums[tid - k] : 0;
-        __syncthreads();
-        sums[tid] += x;
-        __syncthreads();
-    }
-    const uint32_t remain = st->remain;
-    uint32_t before = sums[tid] - total;
-    __syncthreads();
-    if (L == 0 && sums[EV_THREADS - 1] < remain) {
-        if (tid == 0)
-            st->all = 1;
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-        if (before < remain && remain <= before + own[j]) {
-            st->prefix = (prefix << BITS) | (uint32_t)(tid * PER + j);
-            st->remain = remain - before;
-        }
-        before += own[j];
+    x = y = 0;
+    for (int w = 0; w < EV_THREADS / WAVE; ++w) {
+        x += red[0][w];
+        y += red[1][w];
     }
 }
 
 __global__ __launch_bounds__(EV_THREADS) void evict_count_kernel(const float *usage,
                                                                  const uint8_t *may_go, int N,
-                                                                 const EvictState *st,
+                                                                 int rows, const uint32_t *hist,
+                                                                 EvictState *states,
                                                                  uint32_t *counts)
 {
     __shared__ uint32_t red[2][EV_THREADS / WAVE];
-    const uint32_t T = st->prefix;
-    const bool all = st->all != 0;
+    const EvictState st = evict_pick<2>(hist, states[1]);
+    if (blockIdx.x == 0 && threadIdx.x == 0)
+        states[2] = st;
+    const uint32_t T = st.prefix;
+    const bool all = st.all != 0;
     uint32_t below = 0, at = 0;
-    const long r0 = (long)blockIdx.x * EV_ROWS;
-    for (long i = r0 + threadIdx.x; i < min(r0 + EV_ROWS, (long)N); i += EV_THREADS) {
-        const uint32_t key = usage_key(usage[i]);
-        const bool in = !may_go || may_go[i] != 0;
-        below += in && (all || key < T);
-        at += in && !all && key == T;
+    const long r0 = (long)blockIdx.x * rows;
+#pragma unroll 4
+    for (int z = 0; z < rows; z += EV_TILE) {
+        const Four f = load_four(usage, may_go, r0 + z + threadIdx.x * 4, N);
+        bool lt[4], eq[4];
+        below_and_at(f, T, all, lt, eq);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            below += lt[e];
+            at += eq[e];
+        }
     }
-    auto add = [](uint32_t x, uint32_t y) { return x + y; };
-    below = wave_reduce(below, add);
-    at = wave_reduce(at, add);
-    const int wave = threadIdx.x >> 6;
-    if ((threadIdx.x & 63) == 0) {
-        red[0][wave] = below;
-        red[1][wave] = at;
-    }
-    __syncthreads();
-    if (threadIdx.x < 2) {
-        uint32_t s = 0;
-        for (int w = 0; w < EV_THREADS / WAVE; ++w)
-            s += red[threadIdx.x][w];
-        counts[blockIdx.x * 2 + threadIdx.x] = s;
+    block_sums(below, at, red);
+    if (threadIdx.x == 0) {
+        counts[blockIdx.x * 2] = below;
+        counts[blockIdx.x * 2 + 1] = at;
     }
 }
 
 __global__ __launch_bounds__(EV_THREADS) void evict_write_kernel(const float *usage,
                                                                  const uint8_t *may_go, int N,
-                                                                 int n, const EvictState *st,
+                                                                 int rows, int n,
+                                                                 const EvictState *st,
                                                                  const uint32_t *counts,
                                                                  int32_t *victims)
 {
     constexpr int NW = EV_THREADS / WAVE;
     __shared__ uint32_t red[2][NW];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const uint32_t T = st->prefix, remain = st->remain;
+    const uint32_t T = st->prefix;   // (states[2])
     const bool all = st->all != 0;
-    auto add = [](uint32_t x, uint32_t y) { return x + y; };
+    const uint32_t remain = all ? 0u : st->remain;
     // rows below T and at T in the blocks before
     uint32_t below = 0, at = 0;
     for (int k = tid; k < (int)blockIdx.x; k += EV_THREADS) {
         below += counts[2 * k];
         at += counts[2 * k + 1];
     }
-    below = wave_reduce(below, add);
-    at = wave_reduce(at, add);
-    if (lane == 0) {
-        red[0][wave] = below;
-        red[1][wave] = at;
-    }
-    __syncthreads();
-    below = at = 0;
-    for (int w = 0; w < NW; ++w) {
-        below += red[0][w];
-        at += red[1][w];
-    }
-    __syncthreads();
-    const long r0 = (long)blockIdx.x * EV_ROWS;
-    for (long i0 = r0; i0 < min(r0 + EV_ROWS, (long)N); i0 += EV_THREADS) {
-        const long i = i0 + tid;
-        const bool in = i < N && (!may_go || may_go[i] != 0);
-        const uint32_t key = in ? usage_key(usage[i]) : 0;
-        const bool lt = in && (all || key < T), eq = in && !all && key == T;
-        const uint64_t bl = ballot(lt), be = ballot(eq), under = (1ull << lane) - 1;
-        if (lane == 0) {
-            red[0][wave] = __popcll(bl);
-            red[1][wave] = __popcll(be);
-        }
-        __syncthreads();
-        uint32_t l0 = below, e0 = at;
-        for (int w = 0; w < NW; ++w) {
-            if (w < wave) {
-                l0 += red[0][w];
-                e0 += red[1][w];
+    block_sums(below, at, red);
+    const bool none = counts[2 * blockIdx.x] == 0 &&
+                      (counts[2 * blockIdx.x + 1] == 0 || at >= remain);
+    const long r0 = (long)blockIdx.x * rows;
+    if (!none) {
+        const uint64_t under = (1ull << lane) - 1;
+        for (int z = 0; z < rows; z += EV_TILE) {
+            const long i = r0 + z + tid * 4;
+            const Four f = load_four(usage, may_go, i, N);
+            bool lt[4], eq[4];
+            below_and_at(f, T, all, lt, eq);
+            // of the wave, and of its lanes before this one
+            uint32_t wl = 0, we = 0, pl = 0, pe = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint64_t bl = ballot(lt[e]), be = ballot(eq[e]);
+                wl += __popcll(bl);
+                we += __popcll(be);
+                pl += __popcll(bl & under);
+                pe += __popcll(be & under);
             }
-            below += red[0][w];
-            at += red[1][w];
+            __syncthreads();
+            if (lane == 0) {
+                red[0][wave] = wl;
+                red[1][wave] = we;
+            }
+            __syncthreads();
+            pl += below;
+            pe += at;
+            for (int w = 0; w < NW; ++w) {
+                if (w < wave) {
+                    pl += red[0][w];
+                    pe += red[1][w];
+                }
+                below += red[0][w];
+                at += red[1][w];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (lt[e] || (eq[e] && pe < remain)) {
+                    const uint32_t pos = pl + min(pe, remain);
+                    if (pos < (uint32_t)n)
+                        victims[pos] = (int32_t)(i + e);
+                }
+                pl += lt[e];
+                pe += eq[e];
+            }
         }
-        l0 += __popcll(bl & under);
-        e0 += __popcll(be & under);
-        if (lt || (eq && e0 < remain)) {
-            const uint32_t pos = l0 + min(e0, all ? 0u : remain);
-            if (pos < (uint32_t)n)
-                victims[pos] = (int32_t)i;
-        }
-        __syncthreads();
     }
     // fewer rows than asked for: no row behind them
-    if (all && blockIdx.x == gridDim.x - 1)
+    if (all && blockIdx.x == gridDim.x - 1) {
         for (long k = (long)below + tid; k < n; k += EV_THREADS)
             victims[k] = -1;
+    }
 }
 
-int evict_blocks(int N) { return (int)(((long)N + EV_ROWS - 1) / EV_ROWS); }
+// Rows of a block: whole tiles, at most EV_BLOCKS blocks.
+int evict_rows(int N)
+{
+    const long per = ((long)N + EV_BLOCKS - 1) / EV_BLOCKS;
+    return (int)((per + EV_TILE - 1) / EV_TILE * EV_TILE);   // (under 2^24)
+}
 
 template <int SDT>
 hipError_t write_rows(int dtype, const RowsArgs &a, int grid, hipStream_t s)
@@ -328,31 +418,32 @@ hipError_t launch_write_rows(int src_dtype, int dtype, const RowsArgs &a, hipStr
                                : write_rows<1>(dtype, a, (int)grid, s);
 }
 
-size_t evict_bytes(int N)
+size_t evict_bytes(int)
 {
-    const size_t b = 256 + 3 * EV_BINS * 4 + (size_t)evict_blocks(N) * 8;
-    return (b + 255) & ~(size_t)255;
+    return 256 + 3 * EV_COPIES * EV_BINS * 4 + EV_BLOCKS * 2 * 4;
 }
 
 hipError_t launch_evict(const float *usage, const uint8_t *may_go, int N, int n, int32_t *victims,
                         void *ws, hipStream_t s)
 {
-    EvictState *st = (EvictState *)ws;
+    EvictState *st = (EvictState *)ws;   // [3]
     uint32_t *hist = (uint32_t *)((uint8_t *)ws + 256);
-    uint32_t *counts = hist + 3 * EV_BINS;
-    const int blocks = evict_blocks(N), wide = blocks < 512 ? blocks : 512;
-    hipLaunchKernelGGL(evict_clear_kernel, dim3((3 * EV_BINS + EV_THREADS - 1) / EV_THREADS),
-                       dim3(EV_THREADS), 0, s, hist, st, (uint32_t)n);
-    hipLaunchKernelGGL(evict_hist_kernel<0>, dim3(wide), dim3(EV_THREADS), 0, s, usage, may_go, N,
-                       hist, st);
-    hipLaunchKernelGGL(evict_hist_kernel<1>, dim3(wide), dim3(EV_THREADS), 0, s, usage, may_go, N,
-                       hist, st);
-    hipLaunchKernelGGL(evict_hist_kernel<2>, dim3(wide), dim3(EV_THREADS), 0, s, usage, may_go, N,
-                       hist, st);
-    hipLaunchKernelGGL(evict_count_kernel, dim3(blocks), dim3(EV_THREADS), 0, s, usage, may_go, N,
-                       st, counts);
-    hipLaunchKernelGGL(evict_write_kernel, dim3(blocks), dim3(EV_THREADS), 0, s, usage, may_go, N,
-                       n, st, counts, victims);
+    uint32_t *counts = hist + 3 * EV_COPIES * EV_BINS;
+    const int rows = evict_rows(N);
+    const dim3 grid((unsigned)(((long)N + rows - 1) / rows)), block(EV_THREADS);
+    static_assert(3 * EV_COPIES * EV_BINS % EV_THREADS == 0, "the clearing grid");
+    hipLaunchKernelGGL(evict_clear_kernel, dim3(3 * EV_COPIES * EV_BINS / EV_THREADS), block, 0, s,
+                       hist);
+    hipLaunchKernelGGL(evict_hist_kernel<0>, grid, block, 0, s, usage, may_go, N, n, rows, hist,
+                       st);
+    hipLaunchKernelGGL(evict_hist_kernel<1>, grid, block, 0, s, usage, may_go, N, n, rows, hist,
+                       st);
+    hipLaunchKernelGGL(evict_hist_kernel<2>, grid, block, 0, s, usage, may_go, N, n, rows, hist,
+                       st);
+    hipLaunchKernelGGL(evict_count_kernel, grid, block, 0, s, usage, may_go, N, rows, hist, st,
+                       counts);
+    hipLaunchKernelGGL(evict_write_kernel, grid, block, 0, s, usage, may_go, N, rows, n, st + 2,
+                       counts, victims);
     return hipGetLastError();
 }
 
