@@ -1,5 +1,5 @@
 // Attention of requests over the labelled bank: the forward pass.
-#include "attend_scan.hpp"
+#include "attend_gemm.hpp"
 
 #include <math.h>
 
@@ -21,14 +21,15 @@ struct AttendArgs {
     const float *qual, *len;
     int M, nks, n_chunks, n_qt;
     long slabs;
-    float *ml;   // [n_chunks][B][2] maximum (in powers of two) and sum of the weights
+    float *ml;   // [n_chunks][B][2] maximum (of t) and sum of the weights
     float *o;    // [n_chunks][n_lt][B][ct * 16] sums of weighted labels
 };
 
 // One workgroup per (share of the bank, tile of NG * 16 requests, tile of CT *
 // 16 label columns); each wave has its own part of the share, its own running
 // maximum and sums, and the waves' are joined in LDS at the end.
-//   scores   a = <q, x> - |q|^2/2 - |x|^2/2 (MFMA), t = c*a
+//   scores   u = <q, x> - |x|^2/2 (MFMA), t = c*u (|q|^2 changes no weight; the
+//            join adds it to lse)
 //   maximum  raised now and then, the sums rescaled when it is
 //   weights  p = 2^(t - maximum), their sum, and sum of p * label as a second
 //            MFMA (fp32, 16 label columns x 16 requests, 4 rows): its operand
@@ -54,18 +55,6 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
     const float c = A.b.c;
 
     load_requests<DT, NG>(A.b, A.nks, q0, qs, wave, n_waves, lane);
-    // once it is there: -|q|^2/2 of this lane's requests
-    float hq[NG];
-    auto ready = [&] {
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            float sum = 0.f;
-            for (int f = 0; f < A.nks * AtElem<DT>::SUB; ++f)
-                sum = sumsq16<DT == AT_F32 ? 0 : 1>(qs[(f * NG + g) * WAVE + lane], sum);
-            hq[g] = -0.5f * rows_reduce(sum, [](float x, float y) { return x + y; });
-        }
-    };
-
     // this lane's label columns
     const float *lab[CT];
     bool lab_ok[CT];
@@ -133,7 +122,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
                     v[r][e][k] = ok && lab_ok[k] ? v[r][e][k] : 0.f;
 #pragma unroll
                 for (int g = 0; g < NG; ++g)
-                    acc[r][g][e] = ok ? acc[r][g][e] + (nh + hq[g]) : -INFINITY;
+                    acc[r][g][e] = ok ? acc[r][g][e] + nh : -INFINITY;
             }
         }
         bool raise = false;
@@ -181,7 +170,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
             }
         __builtin_amdgcn_sched_barrier(0);
     };
-    scan_slabs<DT, NG, RT, at_ring(DT, RT), false>(A.b, A.nks, qs, s0, s1, lane, ready, side, end);
+    scan_slabs<DT, NG, RT, at_ring(DT, RT), false>(A.b, A.nks, qs, s0, s1, lane, [] {}, side, end);
 
     // ---- the waves' sums, joined (the request tile's LDS is free now)
     constexpr int W = 2 + 16 * CT;
@@ -224,16 +213,209 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
     }
 }
 
+// The same as a matrix product of tiles (attend_gemm.hpp), for large bf16
+// batches and 16 label columns. The weighted labels are products of bf16
+// MFMA too: p as two bf16 values (hi + lo = p to 2^-17), a label as three
+// (exact), five products of 16 columns x 16 requests x 32 rows in place of
+// eight fp32 ones that take twice as long each. The sum of the weights is that
+// of hi + lo, a column of ones: it stands behind the labels (ONES false: at
+// column 2 M), or, where they fill all 16 columns, is two products more.
+template <bool ONES>
+__global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const AttendArgs A)
+{
+    extern __shared__ __align__(16) uint8_t smem[];
+    uint8_t *ring = smem;
+    i32x4 *vf = (i32x4 *)(smem + 2 * AG_SLOT);          // [8][3][64] labels, 32 rows each
+    float *nhs = (float *)(smem + 2 * AG_SLOT + 8 * 3 * WAVE * 16);   // [256] -|x|^2/2
+    int t, ch;
+    chunk_and_tile(A.n_chunks, A.n_qt, &ch, &t);
+    if (ch >= A.n_chunks)
+        return;
+    const int tid = threadIdx.x, lane = tid & 63;
+    __builtin_assume(tid < AT_WAVES * WAVE);
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 15, jg = lane >> 4;
+    const int wr = wave >> 2, wq = wave & 3;
+    const int q0 = t * AG_REQS, lt = blockIdx.y;
+    const long t0 = (long)ch * A.slabs / A.n_chunks, t1 = (long)(ch + 1) * A.slabs / A.n_chunks;
+    const int N = A.b.N, M = A.M;
+    const float c = A.b.c;
+    const int cc = lt * 16 + col;
+    const bool lab_ok = cc < 2 * M;
+    const float *lab = cc < M ? A.qual + cc : lab_ok ? A.len + (cc - M) : A.qual;
+    const bool one = !ONES && lt == 0 && cc == 2 * M;
+
+    float ref[AG_NG], sub[AG_NG];
+    f32x4 o[AG_NG], ol[ONES ? AG_NG : 1];
+#pragma unroll
+    for (int g = 0; g < AG_NG; ++g) {
+        ref[g] = -INFINITY;
+        sub[g] = 0.f;
+        o[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+        ol[ONES ? g : 0] = o[g];
+    }
+    // of a tile: labels of column cc in rows 32*wave + 16*(j/4) + 4*jg + j%4,
+    // norms of row tid, masks of both
+    float v[8], nrm;
+    uint8_t mk[9];
+    const bool masked = A.b.mask != nullptr;
+    auto row_of = [&](int j) { return 32 * wave + (j >> 2) * 16 + 4 * jg + (j & 3); };
+    auto first = [&](int tile) {
+        const long r0 = (t0 + tile) * AG_ROWS;
+        nrm = A.b.norms[min(r0 + (tid & 255), (long)N - 1)];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v[j] = lab[(size_t)min(r0 + row_of(j), (long)N - 1) * M];
+        if (masked) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                mk[j] = A.b.mask[min(r0 + row_of(j), (long)N - 1)];
+            mk[8] = A.b.mask[min(r0 + (tid & 255), (long)N - 1)];
+        }
+    };
+    auto then = [&](int tile) {
+        const long r0 = (t0 + tile) * AG_ROWS;
+        if (tid < AG_ROWS)
+            nhs[tid] = r0 + tid < N && !(masked && mk[8] == 0) ? -0.5f * nrm : -INFINITY;
+        bf16x8 h, m, l;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool ok = lab_ok && r0 + row_of(j) < N && !(masked && mk[j] == 0);
+            const float x = one ? 1.f : ok ? v[j] : 0.f;
+            h[j] = (__bf16)x;
+            const float x1 = x - (float)h[j];
+            m[j] = (__bf16)x1;
+            l[j] = (__bf16)(x1 - (float)m[j]);
+        }
+        i32x4 *at = vf + wave * 3 * WAVE + lane;
+        at[0] = __builtin_bit_cast(i32x4, h);
+        at[WAVE] = __builtin_bit_cast(i32x4, m);
+        at[2 * WAVE] = __builtin_bit_cast(i32x4, l);
+    };
+    auto end = [&](int, f32x4(&acc)[AG_RT][AG_NG]) {
+        const float *nh = nhs + 128 * wr + 4 * jg;
+        bool raise = false;
+        float top[AG_NG];
+#pragma unroll
+        for (int g = 0; g < AG_NG; ++g)
+            top[g] = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < AG_RT; ++r) {
+            __builtin_amdgcn_sched_barrier(0);
+            const f32x4 n4 = *(const f32x4 *)(nh + 16 * r);
+#pragma unroll
+            for (int g = 0; g < AG_NG; ++g) {
+                f32x4 u = acc[r][g] + n4;
+                if (masked)   // (a masked row may hold anything)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        u[e] = n4[e] == -INFINITY ? -INFINITY : u[e];
+                acc[r][g] = u;
+                top[g] = fmaxf(top[g], max4(u));
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < AG_NG; ++g)
+            raise |= c * top[g] > ref[g] + AT_SLACK;
+        if (ballot(raise)) {
+#pragma unroll
+            for (int g = 0; g < AG_NG; ++g) {
+                const float m =
+                    rows_reduce(c * top[g], [](float x, float y) { return fmaxf(x, y); });
+                const float up = fmaxf(ref[g], m);
+                const float f = ref[g] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[g] - up);
+                ref[g] = up;
+                sub[g] = up == -INFINITY ? 0.f : up;
+                o[g] *= f;
+                if constexpr (ONES)
+                    ol[g] *= f;
+            }
+        }
+        const bf16x8 ones = bf16x8{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+#pragma unroll
+        for (int r = 0; r < AG_RT; r += 2) {
+            const i32x4 *at = vf + (4 * wr + r / 2) * 3 * WAVE + lane;
+            const i32x4 vh = at[0], vm = at[WAVE], vl = at[2 * WAVE];
+#pragma unroll
+            for (int g = 0; g < AG_NG; ++g) {
+                __builtin_amdgcn_sched_barrier(0);
+                bf16x8 hi, lo;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float p =
+                        __builtin_amdgcn_exp2f(fmaf(c, acc[r + (j >> 2)][g][j & 3], -sub[g]));
+                    hi[j] = (__bf16)p;
+                    lo[j] = (__bf16)(p - (float)hi[j]);
+                }
+                const i32x4 ph = __builtin_bit_cast(i32x4, hi), pl = __builtin_bit_cast(i32x4, lo);
+                o[g] = mfma_step<1>(vh, ph, o[g]);
+                o[g] = mfma_step<1>(vm, ph, o[g]);
+                o[g] = mfma_step<1>(vl, ph, o[g]);
+                o[g] = mfma_step<1>(vh, pl, o[g]);
+                o[g] = mfma_step<1>(vm, pl, o[g]);
+                if constexpr (ONES) {
+                    ol[g] = mfma_step<1>(__builtin_bit_cast(i32x4, ones), ph, ol[g]);
+                    ol[g] = mfma_step<1>(__builtin_bit_cast(i32x4, ones), pl, ol[g]);
+                }
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    gemm_tiles<false>(A.b, A.nks, ring, q0, t0, (int)(t1 - t0), wave, lane, first, then, end);
+
+    // ---- the two halves of the rows joined: maximum, then 16 columns (and the
+    // sum of the weights, where it is none of them)
+    constexpr int W = 18;
+    float *jn = (float *)smem;   // [2][256][W]
+    stream_barrier();
+#pragma unroll
+    for (int g = 0; g < AG_NG; ++g) {
+        float *at = jn + (wr * AG_REQS + 64 * wq + 16 * g + col) * W;
+        if (jg == 0) {
+            at[0] = ref[g];
+            if constexpr (ONES)
+                at[1] = ol[g][0];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            at[2 + 4 * jg + e] = o[g][e];
+            if (!ONES && 4 * jg + e == 2 * M)
+                at[1] = o[g][e];
+        }
+    }
+    stream_barrier();
+    for (int i = tid; i < AG_REQS * (W - 1); i += AT_WAVES * WAVE) {
+        const int q = i / (W - 1), x = i - q * (W - 1);
+        if (q0 + q >= A.b.B)
+            continue;
+        const float *a = jn + q * W, *b = a + AG_REQS * W;
+        const float m = fmaxf(a[0], b[0]);
+        float sum = 0.f;
+        if (a[0] != -INFINITY)
+            sum = __builtin_amdgcn_exp2f(a[0] - m) * a[1 + x];
+        if (b[0] != -INFINITY)
+            sum = fmaf(__builtin_amdgcn_exp2f(b[0] - m), b[1 + x], sum);
+        if (x > 0) {
+            A.o[(((size_t)ch * gridDim.y + lt) * A.b.B + q0 + q) * 16 + x - 1] = sum;
+        } else if (lt == 0) {
+            float *ml = A.ml + ((size_t)ch * A.b.B + q0 + q) * 2;
+            ml[0] = m;
+            ml[1] = sum;
+        }
+    }
+}
+
 // The shares' sums joined: one workgroup of 256 threads per request, 256 shares
 // at a time. What bounds it is latency: a share's maximum and sum, and the
 // columns (16 at a time, 16 shares side by side), are all sent for before the
 // first is used.
 __global__ __launch_bounds__(256) void attend_join_kernel(const float *ml, const float *o,
                                                           int n_chunks, int n_lt, int width, int B,
-                                                          int M, float *q_hat, float *l_hat,
-                                                          float *lse)
+                                                          int M, const uint8_t *queries, int qbytes,
+                                                          bool bf16, float c, float *q_hat,
+                                                          float *l_hat, float *lse)
 {
-    __shared__ float red[256], wts[256], part[2][4];
+    __shared__ float red[256], wts[256], part[3][4];
     const int b = blockIdx.x, tid = threadIdx.x, wave = tid >> 6;
     const int col = tid & 15, row = tid >> 4;
     // the block's maximum or sum of one value a thread
@@ -263,6 +445,12 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const float *ml, const
         }
     };
     float x[16];
+    float q2 = 0.f;
+    if (lse)
+        for (int at = tid * 16; at < qbytes; at += 256 * 16) {
+            const i32x4 q = load16(queries + (size_t)b * qbytes + at);
+            q2 = bf16 ? sumsq16<1>(q, q2) : sumsq16<0>(q, q2);
+        }
     f32x2 mine = pair(tid);
     columns(0, 0, x);
     float m = mine[0];
@@ -279,8 +467,13 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const float *ml, const
         sum = fmaf(weight(p[0]), p[1], sum);
     }
     const float total = over(1, sum, [](float u, float v) { return u + v; }, 0.f);
-    if (tid == 0 && lse)
-        lse[b] = (m + __builtin_amdgcn_logf(total)) * LN2;
+    if (lse) {
+        // the maximum and c*|q|^2/2 nearly cancel: in 64 bits
+        q2 = over(2, q2, [](float u, float v) { return u + v; }, 0.f);
+        if (tid == 0)
+            lse[b] = (float)((double)m - 0.5 * (double)c * (double)q2 +
+                             (double)__builtin_amdgcn_logf(total)) * LN2;
+    }
     for (int c0 = 0; c0 < 2 * M; c0 += 16) {
         float s = 0.f;
         for (int k0 = 0; k0 < n_chunks; k0 += 256) {
@@ -338,6 +531,18 @@ hipError_t launch_ng(const AttendPlan &p, const AttendArgs &a, hipStream_t s)
     return hipErrorInvalidValue;
 }
 
+hipError_t launch_gemm(const AttendPlan &p, const AttendArgs &a, hipStream_t s)
+{
+    auto kern = 2 * a.M < 16 ? attend_gemm_kernel<false> : attend_gemm_kernel<true>;
+    const hipError_t e = hipFuncSetAttribute(
+        (const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.lds_bytes);
+    if (e != hipSuccess)
+        return e;
+    hipLaunchKernelGGL(kern, dim3(p.n_chunks * p.n_qt, p.n_lt), dim3(AT_WAVES * WAVE), p.lds_bytes,
+                       s, a);
+    return hipGetLastError();
+}
+
 template <int DT>
 hipError_t launch_dt(const AttendPlan &p, const AttendArgs &a, hipStream_t s)
 {
@@ -353,6 +558,23 @@ bool plan_attend(int B, int N, int d, int dtype, int M, int n_cu, AttendPlan *p)
     const int ks = at_ks(dtype);
     p->dtype = dtype;
     p->nks = (d + ks - 1) / ks;
+    p->gemm = at_gemm(dtype, B, N, d);
+    if (p->gemm) {
+        p->nks = (d + AG_K - 1) / AG_K;
+        p->ct = 1;
+        p->n_lt = (2 * M + 15) / 16;
+        p->ng = 16;
+        p->n_qt = (B + AG_REQS - 1) / AG_REQS;
+        p->slabs = (int)(((long)N + AG_ROWS - 1) / AG_ROWS);
+        const int most = n_cu / (p->n_qt * p->n_lt);
+        p->n_chunks = most < 1 ? 1 : most < p->slabs ? most : p->slabs;
+        p->waves = AT_WAVES;
+        p->lds_bytes = 2 * AG_SLOT + 8 * 3 * WAVE * 16 + AG_ROWS * 4;
+        p->off_ml = 0;
+        p->off_o = up256((size_t)p->n_chunks * B * 2 * 4);
+        p->bytes = p->off_o + up256((size_t)p->n_chunks * p->n_lt * B * 16 * 4);
+        return true;
+    }
     p->ct = 2 * M <= 16 ? 1 : 2;
     p->n_lt = (2 * M + 16 * p->ct - 1) / (16 * p->ct);
     const size_t group = (size_t)p->nks * ks * (dtype == AT_F32 ? 4 : 2) * 16;
@@ -403,13 +625,15 @@ hipError_t launch_attend(const AttendPlan &p, const AttendBank &b, const float *
     a.slabs = p.slabs;
     a.ml = (float *)((uint8_t *)ws + p.off_ml);
     a.o = (float *)((uint8_t *)ws + p.off_o);
-    const hipError_t e = p.dtype == AT_F32    ? launch_dt<AT_F32>(p, a, s)
+    const hipError_t e = p.gemm               ? launch_gemm(p, a, s)
+                         : p.dtype == AT_F32  ? launch_dt<AT_F32>(p, a, s)
                          : p.dtype == AT_BF16 ? launch_dt<AT_BF16>(p, a, s)
                                               : launch_dt<AT_Q4>(p, a, s);
     if (e != hipSuccess)
         return e;
     hipLaunchKernelGGL(attend_join_kernel, dim3(b.B), dim3(256), 0, s, a.ml, a.o, p.n_chunks,
-                       p.n_lt, 16 * p.ct, b.B, M, q_hat, l_hat, lse);
+                       p.n_lt, 16 * p.ct, b.B, M, b.queries, (int)at_query_bytes(p.dtype, b.d),
+                       p.dtype != AT_F32, b.c, q_hat, l_hat, lse);
     return hipGetLastError();
 }
 

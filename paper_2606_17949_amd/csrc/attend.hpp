@@ -28,6 +28,7 @@ struct AttendBank {
 };
 
 struct AttendPlan {
+    bool gemm;             // as a matrix product of tiles
     int dtype, ng;         // request tile: ng groups of 16
     int n_qt, n_chunks;    // request tiles, shares of the bank
     int waves, nks;        // waves of a workgroup, k-steps of a row
@@ -37,6 +38,12 @@ struct AttendPlan {
     size_t lds_bytes;
     size_t off_ml, off_o, bytes;   // workspace: partial maxima and sums, partial averages
 };
+
+// Whether a batch goes by as a matrix product of tiles (attend_gemm.hpp).
+inline bool at_gemm(int dtype, int B, int, int d)
+{
+    return dtype == AT_BF16 && B > 64 && d >= 128;
+}
 
 // The forward pass on a device of n_cu compute units; false if no layout fits.
 bool plan_attend(int B, int N, int d, int dtype, int M, int n_cu, AttendPlan *p);

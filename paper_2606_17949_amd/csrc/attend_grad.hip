@@ -571,7 +571,7 @@ __global__ __launch_bounds__(512, 1) void dx_kernel(const DxArgs A)
 {
     constexpr int H = DT == AT_BF16 ? 2 : 1;   // values of ds
     constexpr int MDT = DT == AT_F32 ? 0 : 1;
-    constexpr int SLOT = DX_MOST * WAVE;       // 16-byte places
+    constexpr int SLOT = (NC + 7) / 8 * 8 * WAVE;       // 16-byte places
     __shared__ __align__(16) i32x4 ring[DX_SLOTS * SLOT];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -592,7 +592,7 @@ __global__ __launch_bounds__(512, 1) void dx_kernel(const DxArgs A)
     const uint32_t place = (uint32_t)ds_place(lane) * 16;
     auto fetch = [&](int blk) {   // two fragments of block blk by this wave
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < (NC + 7) / 8; ++j) {
             const int f = wave + 8 * j;
             dma16(rq, ring + (blk % DX_SLOTS) * SLOT + f * WAVE,
                   blk < A.n_blk && f < NC && dt0 + f < A.n_dt
@@ -631,7 +631,7 @@ __global__ __launch_bounds__(512, 1) void dx_kernel(const DxArgs A)
             // this wave's part of the block and its ds are there once only what
             // was sent after them is outstanding; after the barrier every wave's
             // part is, and no wave reads the slot of the block before any more
-            wait_vmcnt<2 + AT_RT * H>();
+            wait_vmcnt<(NC + 7) / 8 + AT_RT * H>();
             stream_barrier();
             fetch(blk + 3);
             __builtin_amdgcn_sched_barrier(0);
@@ -670,17 +670,37 @@ __global__ __launch_bounds__(512, 1) void dx_kernel(const DxArgs A)
             sum += A.rowsum[(size_t)t * A.part_rows + lr];
         const size_t row = (size_t)(A.row0 + lr);
         const bool live = !A.mask || A.mask[row] != 0;
+        // (eight columns a lane: 16 rows x 64 bytes an instruction of bf16; four at a
+        // time took 160 us for FIXDX at 256 x 100,000 x 768)
 #pragma unroll
-        for (int k = 0; k < NC; ++k) {
+        for (int k = 0; k < NC; k += 2) {
             const int c0 = dealt_column(dt0 + k, 4 * jg);
             if (c0 >= A.d)
                 continue;
-            const f32x4 x = load4<DT>(A.rows, row * A.d + c0);
-            f32x4 v;
+            const size_t at = row * A.d + c0;
+            f32x4 v[2];
+            auto result = [&](int h, const f32x4 &x) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] = live ? A.scale * (acc[r][k][e] - x[e] * sum) : 0.f;
-            store4<DT>(A.d_bank, row * A.d + c0, v);
+                for (int e = 0; e < 4; ++e)
+                    v[h][e] = live ? A.scale * (acc[r][k + h][e] - x[e] * sum) : 0.f;
+            };
+            if constexpr (DT == AT_BF16) {
+                const i32x4 x = load16(A.rows + at * 2);
+                result(0, f32x4{bf16lo(x[0]), bf16hi(x[0]), bf16lo(x[1]), bf16hi(x[1])});
+                result(1, f32x4{bf16lo(x[2]), bf16hi(x[2]), bf16lo(x[3]), bf16hi(x[3])});
+                bf16x8 y;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    y[e] = (__bf16)v[e >> 2][e & 3];
+                *(bf16x8 *)(A.d_bank + at * 2) = y;
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (c0 + 4 * h < A.d) {
+                        result(h, load4<DT>(A.rows, at + 4 * h));
+                        store4<DT>(A.d_bank, at + 4 * h, v[h]);
+                    }
+            }
         }
     }
 }
@@ -1100,7 +1120,7 @@ hipError_t run_grad(const GradPlan &p, const AttendBank &b, const GradArgs &g, u
             // as many columns to a workgroup as leave few of the last one's idle
             const int per = (n_dt + (n_dt + DX_MOST - 1) / DX_MOST - 1) /
                             ((n_dt + DX_MOST - 1) / DX_MOST);
-            e = per > 12 ? dx_one<DT, 16>(x, s) : per > 8 ? dx_one<DT, 12>(x, s) : dx_one<DT, 8>(x, s);
+            e = dx_one<DT, 8>(x, s);
             if (e != hipSuccess)
                 return e;
         }
