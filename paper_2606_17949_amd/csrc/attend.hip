@@ -220,13 +220,15 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
 // eight fp32 ones that take twice as long each. The sum of the weights is that
 // of hi + lo, a column of ones: it stands behind the labels (ONES false: at
 // column 2 M), or, where they fill all 16 columns, is two products more.
+constexpr int ONE2 = 0x3f803f80;   // two bf16 ones
+
 template <bool ONES>
 __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const AttendArgs A)
 {
     extern __shared__ __align__(16) uint8_t smem[];
     uint8_t *ring = smem;
-    i32x4 *vf = (i32x4 *)(smem + 2 * AG_SLOT);          // [8][3][64] labels, 32 rows each
-    float *nhs = (float *)(smem + 2 * AG_SLOT + 8 * 3 * WAVE * 16);   // [256] -|x|^2/2
+    float *labels = (float *)(smem + 2 * AG_SLOT);   // [64][64]
+    TileSide *side = (TileSide *)(labels + 64 * WAVE);
     int t, ch;
     chunk_and_tile(A.n_chunks, A.n_qt, &ch, &t);
     if (ch >= A.n_chunks)
@@ -240,10 +242,15 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
     const long t0 = (long)ch * A.slabs / A.n_chunks, t1 = (long)(ch + 1) * A.slabs / A.n_chunks;
     const int N = A.b.N, M = A.M;
     const float c = A.b.c;
+    // the lane's label column (16 to a tile; behind the last, the first again)
     const int cc = lt * 16 + col;
-    const bool lab_ok = cc < 2 * M;
-    const float *lab = cc < M ? A.qual + cc : lab_ok ? A.len + (cc - M) : A.qual;
+    const float *lab = cc < M ? A.qual + cc : cc < 2 * M ? A.len + (cc - M) : A.qual;
     const bool one = !ONES && lt == 0 && cc == 2 * M;
+    // piece 8*b + 4*h + e: rows 32*b + 16*h + 4*(lane/16) + e
+    auto label = [&](long row0, int f, int l) {
+        const long row = row0 + (f >> 3) * 32 + ((f >> 2) & 1) * 16 + 4 * (l >> 4) + (f & 3);
+        return lab + (size_t)min(row, (long)N - 1) * M;
+    };
 
     float ref[AG_NG], sub[AG_NG];
     f32x4 o[AG_NG], ol[ONES ? AG_NG : 1];
@@ -254,46 +261,9 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
         o[g] = f32x4{0.f, 0.f, 0.f, 0.f};
         ol[ONES ? g : 0] = o[g];
     }
-    // of a tile: labels of column cc in rows 32*wave + 16*(j/4) + 4*jg + j%4,
-    // norms of row tid, masks of both
-    float v[8], nrm;
-    uint8_t mk[9];
     const bool masked = A.b.mask != nullptr;
-    auto row_of = [&](int j) { return 32 * wave + (j >> 2) * 16 + 4 * jg + (j & 3); };
-    auto first = [&](int tile) {
-        const long r0 = (t0 + tile) * AG_ROWS;
-        nrm = A.b.norms[min(r0 + (tid & 255), (long)N - 1)];
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            v[j] = lab[(size_t)min(r0 + row_of(j), (long)N - 1) * M];
-        if (masked) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                mk[j] = A.b.mask[min(r0 + row_of(j), (long)N - 1)];
-            mk[8] = A.b.mask[min(r0 + (tid & 255), (long)N - 1)];
-        }
-    };
-    auto then = [&](int tile) {
-        const long r0 = (t0 + tile) * AG_ROWS;
-        if (tid < AG_ROWS)
-            nhs[tid] = r0 + tid < N && !(masked && mk[8] == 0) ? -0.5f * nrm : -INFINITY;
-        bf16x8 h, m, l;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const bool ok = lab_ok && r0 + row_of(j) < N && !(masked && mk[j] == 0);
-            const float x = one ? 1.f : ok ? v[j] : 0.f;
-            h[j] = (__bf16)x;
-            const float x1 = x - (float)h[j];
-            m[j] = (__bf16)x1;
-            l[j] = (__bf16)(x1 - (float)m[j]);
-        }
-        i32x4 *at = vf + wave * 3 * WAVE + lane;
-        at[0] = __builtin_bit_cast(i32x4, h);
-        at[WAVE] = __builtin_bit_cast(i32x4, m);
-        at[2 * WAVE] = __builtin_bit_cast(i32x4, l);
-    };
-    auto end = [&](int, f32x4(&acc)[AG_RT][AG_NG]) {
-        const float *nh = nhs + 128 * wr + 4 * jg;
+    auto end = [&](int tile, f32x4(&acc)[AG_RT][AG_NG]) {
+        const int left = (int)min((long)AG_ROWS, N - (t0 + tile) * AG_ROWS);
         bool raise = false;
         float top[AG_NG];
 #pragma unroll
@@ -302,7 +272,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
 #pragma unroll
         for (int r = 0; r < AG_RT; ++r) {
             __builtin_amdgcn_sched_barrier(0);
-            const f32x4 n4 = *(const f32x4 *)(nh + 16 * r);
+            const f32x4 n4 = tile_norms(A.b, side, left, 128 * wr + 16 * r + 4 * jg);
 #pragma unroll
             for (int g = 0; g < AG_NG; ++g) {
                 f32x4 u = acc[r][g] + n4;
@@ -331,37 +301,63 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
                     ol[g] *= f;
             }
         }
-        const bf16x8 ones = bf16x8{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+        const i32x4 ones = i32x4{ONE2, ONE2, ONE2, ONE2};
 #pragma unroll
         for (int r = 0; r < AG_RT; r += 2) {
-            const i32x4 *at = vf + (4 * wr + r / 2) * 3 * WAVE + lane;
-            const i32x4 vh = at[0], vm = at[WAVE], vl = at[2 * WAVE];
+            __builtin_amdgcn_sched_barrier(0);
+            // the labels of these 32 rows as three bf16 values each (those of rows
+            // without weight may be no numbers: made finite)
+            i32x4 vh, vm, vl;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float x[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float y = labels[(8 * (4 * wr + r / 2) + 2 * j + i) * WAVE + lane];
+                    x[i] = one ? 1.f : __builtin_amdgcn_fmed3f(y, -3e38f, 3e38f);
+                }
+                vh[j] = split_bf16(x[0], x[1]);
+                vm[j] = split_bf16(x[0], x[1]);
+                vl[j] = split_bf16(x[0], x[1]);
+            }
+            i32x4 ph[AG_NG], pl[AG_NG];
 #pragma unroll
             for (int g = 0; g < AG_NG; ++g) {
-                __builtin_amdgcn_sched_barrier(0);
-                bf16x8 hi, lo;
+                if (g == 2)
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float p =
-                        __builtin_amdgcn_exp2f(fmaf(c, acc[r + (j >> 2)][g][j & 3], -sub[g]));
-                    hi[j] = (__bf16)p;
-                    lo[j] = (__bf16)(p - (float)hi[j]);
+                for (int j = 0; j < 4; ++j) {
+                    const f32x4 &u = acc[r + (j >> 1)][g];
+                    float x = __builtin_amdgcn_exp2f(fmaf(c, u[2 * (j & 1)], -sub[g]));
+                    float y = __builtin_amdgcn_exp2f(fmaf(c, u[2 * (j & 1) + 1], -sub[g]));
+                    ph[g][j] = split_bf16(x, y);
+                    pl[g][j] = split_bf16(x, y);
                 }
-                const i32x4 ph = __builtin_bit_cast(i32x4, hi), pl = __builtin_bit_cast(i32x4, lo);
-                o[g] = mfma_step<1>(vh, ph, o[g]);
-                o[g] = mfma_step<1>(vm, ph, o[g]);
-                o[g] = mfma_step<1>(vl, ph, o[g]);
-                o[g] = mfma_step<1>(vh, pl, o[g]);
-                o[g] = mfma_step<1>(vm, pl, o[g]);
-                if constexpr (ONES) {
-                    ol[g] = mfma_step<1>(__builtin_bit_cast(i32x4, ones), ph, ol[g]);
-                    ol[g] = mfma_step<1>(__builtin_bit_cast(i32x4, ones), pl, ol[g]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            // (product by product over the groups: no product waits for the one before)
+            auto weigh = [&](const i32x4 &v, const i32x4(&p)[AG_NG], f32x4(&to)[AG_NG]) {
+#pragma unroll
+                for (int g = 0; g < AG_NG; ++g)
+                    to[g] = mfma_step<1>(v, p[g], to[g]);
+            };
+            weigh(vh, ph, o);
+            weigh(vm, ph, o);
+            weigh(vl, ph, o);
+            weigh(vh, pl, o);
+            weigh(vm, pl, o);
+            if constexpr (ONES) {
+#pragma unroll
+                for (int g = 0; g < AG_NG; ++g) {
+                    ol[g] = mfma_step<1>(ones, ph[g], ol[g]);
+                    ol[g] = mfma_step<1>(ones, pl[g], ol[g]);
                 }
             }
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    gemm_tiles<false>(A.b, A.nks, ring, q0, t0, (int)(t1 - t0), wave, lane, first, then, end);
+    gemm_tiles<AG_RT, false, 8>(A.b, A.nks, ring, side, labels, q0, t0, (int)(t1 - t0), wave, lane,
+                             label, end);
 
     // ---- the two halves of the rows joined: maximum, then 16 columns (and the
     // sum of the weights, where it is none of them)
@@ -569,7 +565,7 @@ bool plan_attend(int B, int N, int d, int dtype, int M, int n_cu, AttendPlan *p)
         const int most = n_cu / (p->n_qt * p->n_lt);
         p->n_chunks = most < 1 ? 1 : most < p->slabs ? most : p->slabs;
         p->waves = AT_WAVES;
-        p->lds_bytes = 2 * AG_SLOT + 8 * 3 * WAVE * 16 + AG_ROWS * 4;
+        p->lds_bytes = 2 * AG_SLOT + 64 * WAVE * 4 + sizeof(TileSide);
         p->off_ml = 0;
         p->off_o = up256((size_t)p->n_chunks * B * 2 * 4);
         p->bytes = p->off_o + up256((size_t)p->n_chunks * p->n_lt * B * 16 * 4);

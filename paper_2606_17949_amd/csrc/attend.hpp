@@ -55,7 +55,9 @@ hipError_t launch_attend(const AttendPlan &p, const AttendBank &a, const float *
 // The accumulated weight of the bank's rows: usage = decay * usage + sum over
 // the batch of p.
 struct UsagePlan {
+    bool gemm;            // as a matrix product of tiles
     int dtype, ng, n_qt, n_chunks, waves, nks, slabs;
+    int n_part;           // partial sums of a row
     size_t lds_bytes;
     size_t off_side, off_part, bytes;   // per request; partial sums per request tile
 };
@@ -73,7 +75,9 @@ hipError_t launch_zero(void *p, size_t bytes, hipStream_t s);   // bytes a multi
 // gradient ds (and what needs no further product), then d_queries += ds * rows,
 // then d_bank = ds^T * queries.
 struct GradPlan {
+    bool gemm;            // the first pass as a matrix product of tiles
     int dtype, ng, n_qt, n_chunks, waves, nks, slabs;
+    int n_gt;             // its request tiles (n_qt: tiles of ng groups, 64 of them a wave's)
     bool tab;             // the label gradients of a request tile fit LDS
     int n_blk;            // blocks of requests of one fragment of ds (32, fp32 16)
     int n_dt;             // fragments of 16 columns of a block of requests

@@ -1,6 +1,6 @@
 // Attention of requests over the labelled bank: the passes that recompute its
 // probabilities, the rows' accumulated weight and the gradients.
-#include "attend_scan.hpp"
+#include "attend_gemm.hpp"
 
 #include <math.h>
 
@@ -206,6 +206,69 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_kernel(const UsageAr
         }
     };
     scan_slabs<DT, NG, RT, at_ring(DT, RT), true>(A.b, A.nks, qs, s0, s1, lane, ready, side, end);
+}
+
+// The same as a matrix product of tiles, for large bf16 batches; part [4 *
+// n_qt][N], one of the waves of each 64 requests.
+__global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_gemm_kernel(const UsageArgs A)
+{
+    extern __shared__ __align__(16) uint8_t smem[];
+    TileSide *side = (TileSide *)(smem + 2 * AG_SLOT);
+    float *sd = (float *)(side + 1);   // [2][256] hq, lse2
+    int t, ch;
+    chunk_and_tile(A.n_chunks, A.n_qt, &ch, &t);
+    if (ch >= A.n_chunks)
+        return;
+    const int tid = threadIdx.x, lane = tid & 63;
+    __builtin_assume(tid < AT_WAVES * WAVE);
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 15, jg = lane >> 4;
+    const int wr = wave >> 2, wq = wave & 3;
+    const int q0 = t * AG_REQS;
+    const long t0 = (long)ch * A.slabs / A.n_chunks, t1 = (long)(ch + 1) * A.slabs / A.n_chunks;
+    const int N = A.b.N;
+    const float c = A.b.c;
+    if (tid < AG_REQS) {
+        const Side x = q0 + tid < A.b.B ? A.side[q0 + tid] : Side{0.f, INFINITY, 0.f, 0.f};
+        sd[tid] = x.hq;
+        sd[AG_REQS + tid] = x.lse2;
+    }
+    const bool any = q0 + 64 * wq < A.b.B;
+    float *const part = A.part + (size_t)(any ? t * 4 + wq : 0) * N;
+    auto end = [&](int tile, f32x4(&acc)[AG_RT][AG_NG]) {
+        const long row0 = (t0 + tile) * AG_ROWS;
+        const int left = (int)min((long)AG_ROWS, N - row0);
+        const __amdgpu_buffer_rsrc_t to = make_rsrc(part + row0, any ? (uint32_t)left * 4u : 0u);
+        float sum[AG_RT];
+#pragma unroll
+        for (int r = 0; r < AG_RT; ++r)
+            sum[r] = 0.f;
+#pragma unroll
+        for (int g = 0; g < AG_NG; ++g) {
+            const float *at = sd + 64 * wq + 16 * g + 4 * jg;
+            const f32x4 hq = *(const f32x4 *)at, lse2 = *(const f32x4 *)(at + AG_REQS);
+#pragma unroll
+            for (int r = 0; r < AG_RT; ++r) {
+                if (r % 2 == 0)
+                    __builtin_amdgcn_sched_barrier(0);
+                const float nh = -0.5f * side->norms[128 * wr + 16 * r + col];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    sum[r] += __builtin_amdgcn_exp2f(
+                        fmaf(c, acc[r][g][e] + (nh + hq[e]), -lse2[e]));
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < AG_RT; ++r) {
+            float s = rows_reduce(sum[r], [](float x, float y) { return x + y; });
+            const int at = 128 * wr + 16 * r + col;
+            // (a masked row may hold anything)
+            s = tile_norm(A.b, side, left, at) == -INFINITY ? 0.f : s;
+            buffer_store4(to, jg == 0 ? (uint32_t)at * 4u : OFF_NONE, s);
+        }
+    };
+    gemm_tiles<AG_RT, true, 0>(A.b, A.nks, smem, side, nullptr, q0, t0, (int)(t1 - t0), wave, lane,
+                        [&](long, int, int) { return A.b.norms; }, end);
 }
 
 __global__ __launch_bounds__(256) void usage_join_kernel(const float *part, int n_qt, int N,
@@ -519,6 +582,213 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_kernel(const DsArgs A)
             s += jn[w * NG * 32 + i];
         float *at = A.req + ((size_t)ch * A.b.B + q0) * 2 + i;
         *at = A.first ? s : *at + s;
+    }
+}
+
+// The same as a matrix product of tiles, for large bf16 batches and at most 16
+// label columns. Request tiles of 64 (a wave's) as above in rowsum and the
+// labels' gradients; the label gradients of the requests stand in LDS as the
+// fragments of dp, [groups][4][64], a tile's labels beside them, [16 row
+// tiles][4][64].
+constexpr int DS_RT = 4;
+
+__global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_gemm_kernel(const DsArgs A)
+{
+    constexpr int REQS = ag_reqs(DS_RT), WQ = REQS / 64;
+    extern __shared__ __align__(16) uint8_t smem[];
+    TileSide *side = (TileSide *)(smem + 2 * ag_slot(DS_RT));
+    float *sd = (float *)(side + 1);         // [3][REQS] hq, lse2, shift
+    float *tab = sd + 3 * REQS;              // [REQS / 16][4][64]
+    float *labels = tab + REQS / 16 * 4 * WAVE;   // [16][4][64]
+    int t, ch;
+    chunk_and_tile(A.n_chunks, A.n_qt, &ch, &t);
+    if (ch >= A.n_chunks)
+        return;
+    const int tid = threadIdx.x, lane = tid & 63;
+    __builtin_assume(tid < AT_WAVES * WAVE);
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 15, jg = lane >> 4;
+    const int wr = wave / WQ, wq = wave % WQ;
+    const int q0 = t * REQS, qw = q0 + 64 * wq, t64 = t * WQ + wq;
+    const bool any = qw < A.b.B;
+    const int n_tiles = (int)((A.slabs + 7) / 8);   // of the part
+    const int t0 = (int)((long)ch * n_tiles / A.n_chunks),
+              t1 = (int)((long)(ch + 1) * n_tiles / A.n_chunks);
+    const int N = A.b.N, M = A.M;
+    const float c = A.b.c;
+    if (tid < REQS) {
+        const Side x = q0 + tid < A.b.B ? A.side[q0 + tid] : Side{0.f, INFINITY, 0.f, 0.f};
+        sd[tid] = x.hq;
+        sd[REQS + tid] = x.lse2;
+        sd[2 * REQS + tid] = x.shift;
+    }
+    for (int i = tid; i < REQS / 16 * 4 * WAVE; i += AT_WAVES * WAVE) {
+        const int q = q0 + (i >> 8) * 16 + (i & 15), cc = ((i >> 6) & 3) * 4 + ((i >> 4) & 3);
+        tab[i] = q < A.b.B ? A.dout[(size_t)q * A.pitch + cc] : 0.f;
+    }
+    const long part0 = A.slab0 * AT_SLAB;   // first row of the part
+    float sum_ds[AG_NG][4], sum_db[AG_NG][4];
+#pragma unroll
+    for (int g = 0; g < AG_NG; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            sum_ds[g][e] = sum_db[g][e] = 0.f;
+    // the lane's address in piece 4*i + j of a tile's labels: row tile i, column
+    // 4*j + jg (behind the last column, the first again)
+    auto label = [&](long row0, int f, int l) {
+        const long row = min(row0 + (f >> 2) * 16 + (l & 15), (long)N - 1);
+        const int cc = 4 * (f & 3) + (l >> 4);
+        return (cc < M || cc >= 2 * M ? A.qual : A.len) + row * M +
+               (cc < M ? cc : cc < 2 * M ? cc - M : 0);
+    };
+    auto end = [&](int tile, f32x4(&acc)[DS_RT][AG_NG]) {
+        const int l = fresh(lane), col = l & 15, jg = l >> 4;
+        // this lane's places in 16 rows of the labels' gradients (columns 4*jg + e of
+        // row col) and in a fragment of ds
+        uint32_t off_q[4], off_l[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int cc = 4 * jg + e;
+            off_q[e] = cc < M ? (uint32_t)(col * M + cc) * 4u : OFF_NONE;
+            off_l[e] = cc >= M && cc < 2 * M ? (uint32_t)(col * M + cc - M) * 4u : OFF_NONE;
+        }
+        const uint32_t place = (uint32_t)ds_place(l) * 16;
+        const long row0 = part0 + (long)(t0 + tile) * AG_ROWS;
+        const int left = (int)min((long)AG_ROWS, N - row0);
+        const long tile16 = (long)(t0 + tile) * 16 + DS_RT * wr;   // of the part's row tiles
+        const int r0 = 16 * DS_RT * wr;   // this wave's rows
+        const size_t lab_at = ((size_t)(any ? t64 : 0) * N + row0 + r0) * M;
+#pragma unroll
+        for (int r = 0; r < DS_RT; ++r) {
+            // (what the requests have in LDS is read again for every row tile: kept
+            // in registers it would not leave room for the scores)
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            const float nh = tile_norm(A.b, side, left, r0 + 16 * r + col);
+            const bool live = nh != -INFINITY;
+            float x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                x[j] = live && 4 * j + jg < 2 * M
+                           ? labels[((DS_RT * wr + r) * 4 + j) * WAVE + l]
+                           : 0.f;
+            f32x4 dp[AG_NG];
+#pragma unroll
+            for (int g = 0; g < AG_NG; ++g)
+                dp[g] = -*(const f32x4 *)(sd + 2 * REQS + 64 * wq + 16 * g + 4 * jg);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (4 * j < 2 * M)
+#pragma unroll
+                    for (int g = 0; g < AG_NG; ++g)
+                        dp[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                            tab[((4 * wq + g) * 4 + j) * WAVE + l], x[j], dp[g], 0, 0, 0);
+            float rs = 0.f;
+#pragma unroll
+            for (int g = 0; g < AG_NG; ++g) {
+                __builtin_amdgcn_sched_barrier(0);
+                const float *s4 = sd + 64 * wq + 16 * g + 4 * jg;
+                const f32x4 hq = *(const f32x4 *)s4, lse2 = *(const f32x4 *)(s4 + REQS);
+                float ds[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float a = live ? acc[r][g][e] + (nh + hq[e]) : 0.f;
+                    const float p = live ? __builtin_amdgcn_exp2f(fmaf(c, a, -lse2[e])) : 0.f;
+                    ds[e] = p * dp[g][e];
+                    acc[r][g][e] = p;
+                    sum_db[g][e] = fmaf(2.f * a, ds[e], sum_db[g][e]);   // -distance = 2 a
+                }
+                int h[2], l[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float y0 = ds[2 * i], y1 = ds[2 * i + 1];
+                    h[i] = split_bf16(y0, y1);
+                    l[i] = split_bf16(y0, y1);
+                    // what the two bf16 values hold: ds less what they leave
+                    const float z0 = ds[2 * i] - y0, z1 = ds[2 * i + 1] - y1;
+                    sum_ds[g][2 * i] += z0;
+                    sum_ds[g][2 * i + 1] += z1;
+                    rs += z0 + z1;
+                }
+                dp[g] = __builtin_bit_cast(f32x4, i32x4{h[0], h[1], l[0], l[1]});
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (A.ds) {
+#pragma unroll
+                for (int g = 0; g < AG_NG; g += 2) {
+                    const int blk = (qw >> 5) + (g >> 1);
+                    const __amdgpu_buffer_rsrc_t to =
+                        wave_rsrc(A.ds + ((tile16 + r) * A.n_blk + min(blk, A.n_blk - 1)) * 2 * WAVE,
+                                  blk < A.n_blk ? 2 * WAVE * 16u : 0u);
+                    const bool turned = col & 4;
+                    const f32x4 u = turned ? dp[g + 1] : dp[g], w = turned ? dp[g] : dp[g + 1];
+                    __builtin_amdgcn_raw_buffer_store_b128(
+                        __builtin_bit_cast(i32x4, f32x4{u[0], u[1], w[0], w[1]}), to, (int)place, 0,
+                        0);
+                    __builtin_amdgcn_raw_buffer_store_b128(
+                        __builtin_bit_cast(i32x4, f32x4{u[2], u[3], w[2], w[3]}), to,
+                        (int)(place + WAVE * 16), 0, 0);
+                }
+                rs = rows_reduce(rs, [](float y, float z) { return y + z; });
+                buffer_store4(wave_rsrc(A.rowsum + (any ? (size_t)t64 * A.part_rows : 0) +
+                                            (tile16 + r) * 16,
+                                        any ? 64u : 0u),
+                              jg == 0 ? (uint32_t)col * 4u : OFF_NONE, rs);
+            }
+            if (A.d_qual || A.d_len) {
+                f32x4 dv = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int g = 0; g < AG_NG; ++g) {
+                    // of label column `col`, this lane's four requests
+                    const f32x4 d4 = *(const f32x4 *)(tab + ((4 * wq + g) * 4 + (col >> 2)) * WAVE +
+                                                      (col & 3) * 16 + 4 * jg);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        dv = __builtin_amdgcn_mfma_f32_16x16x4f32(d4[e], acc[r][g][e], dv, 0, 0,
+                                                                  0);
+                }
+                const uint32_t rows = any ? (uint32_t)max(0, min(16, left - r0 - 16 * r)) : 0u;
+                const __amdgpu_buffer_rsrc_t to_q =
+                    wave_rsrc((A.d_qual ? A.d_qual : A.d_len) + lab_at + 16 * r * M,
+                              A.d_qual ? rows * M * 4u : 0u);
+                const __amdgpu_buffer_rsrc_t to_l =
+                    wave_rsrc((A.d_len ? A.d_len : A.d_qual) + lab_at + 16 * r * M,
+                              A.d_len ? rows * M * 4u : 0u);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    buffer_store4(to_q, off_q[e], dv[e]);
+                    buffer_store4(to_l, off_l[e], dv[e]);
+                }
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    gemm_tiles<DS_RT, true, 8>(A.b, A.nks, smem, side, labels, q0, A.slab0 / 8 + t0, t1 - t0, wave,
+                               lane, label, end);
+
+    // ---- the requests' sums, joined over the waves of a request
+    float *jn = (float *)smem;   // [8 / WQ][REQS][2]
+    stream_barrier();
+#pragma unroll
+    for (int g = 0; g < AG_NG; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            auto add = [](float x, float y) { return x + y; };
+            const float x = row16_reduce(sum_ds[g][e], add), y = row16_reduce(sum_db[g][e], add);
+            if (col == 0) {
+                float *to = jn + (wr * REQS + 64 * wq + 16 * g + 4 * jg + e) * 2;
+                to[0] = x;
+                to[1] = y;
+            }
+        }
+    stream_barrier();
+    const int i = tid;   // request i/2, sum i%2
+    if (i < 2 * REQS && q0 + i / 2 < A.b.B) {
+        float s = 0.f;
+        for (int w = 0; w < AT_WAVES / WQ; ++w)
+            s += jn[w * 2 * REQS + i];
+        float *to = A.req + ((size_t)ch * A.b.B + q0) * 2 + i;
+        *to = A.first ? s : *to + s;
     }
 }
 
@@ -986,6 +1256,16 @@ hipError_t usage_one(const UsagePlan &p, const UsageArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
+hipError_t usage_gemm(const UsagePlan &p, const UsageArgs &a, hipStream_t s)
+{
+    const hipError_t e = allow_lds(usage_gemm_kernel, p.lds_bytes);
+    if (e != hipSuccess)
+        return e;
+    hipLaunchKernelGGL(usage_gemm_kernel, dim3(p.n_chunks * p.n_qt), dim3(AT_WAVES * WAVE),
+                       p.lds_bytes, s, a);
+    return hipGetLastError();
+}
+
 template <int DT>
 hipError_t usage_dt(const UsagePlan &p, const UsageArgs &a, hipStream_t s)
 {
@@ -1005,6 +1285,16 @@ hipError_t ds_one(const GradPlan &p, const DsArgs &a, hipStream_t s)
     if (e != hipSuccess)
         return e;
     hipLaunchKernelGGL(kern, dim3(p.n_chunks * p.n_qt), dim3(p.waves * WAVE), p.lds_bytes, s, a);
+    return hipGetLastError();
+}
+
+hipError_t ds_gemm(const GradPlan &p, const DsArgs &a, hipStream_t s)
+{
+    const hipError_t e = allow_lds(ds_gemm_kernel, p.lds_bytes);
+    if (e != hipSuccess)
+        return e;
+    hipLaunchKernelGGL(ds_gemm_kernel, dim3(p.n_chunks * p.n_gt), dim3(AT_WAVES * WAVE),
+                       p.lds_bytes, s, a);
     return hipGetLastError();
 }
 
@@ -1079,7 +1369,7 @@ hipError_t run_grad(const GradPlan &p, const AttendBank &b, const GradArgs &g, u
     a.pitch = p.pitch;
     a.nks = p.nks;
     a.n_chunks = p.n_chunks;
-    a.n_qt = p.n_qt;
+    a.n_qt = p.gemm ? p.n_gt : p.n_qt;
     a.n_blk = p.n_blk;
     a.ds = g.d_queries || g.d_bank ? (i32x4 *)(wb + p.off_ds) : nullptr;
     a.rowsum = (float *)(wb + p.off_rowsum);
@@ -1098,7 +1388,7 @@ hipError_t run_grad(const GradPlan &p, const AttendBank &b, const GradArgs &g, u
         a.slab0 = z0;
         a.slabs = slabs;
         a.first = z0 == 0;
-        if ((e = ds_dt<DT>(p, a, s)) != hipSuccess)
+        if ((e = p.gemm ? ds_gemm(p, a, s) : ds_dt<DT>(p, a, s)) != hipSuccess)
             return e;
         if (g.d_queries) {
             DqArgs q{a.ds, b.rows, b.mask, b.B, b.d, p.n_blk, p.q_chunks, row0, nrows, slabs, dq,
@@ -1150,6 +1440,20 @@ bool plan_usage(int B, int N, int d, int dtype, int n_cu, UsagePlan *p)
     const int ks = at_ks(dtype);
     p->dtype = dtype;
     p->nks = (d + ks - 1) / ks;
+    p->gemm = at_gemm(dtype, B, N, d);
+    p->off_side = 0;
+    p->off_part = up256((size_t)B * sizeof(Side));
+    if (p->gemm) {
+        p->nks = (d + AG_K - 1) / AG_K;
+        p->n_qt = (B + AG_REQS - 1) / AG_REQS;
+        p->n_part = (B + 63) / 64;
+        p->slabs = (int)(((long)N + AG_ROWS - 1) / AG_ROWS);
+        const int most = n_cu / p->n_qt;
+        p->n_chunks = most < 1 ? 1 : most < p->slabs ? most : p->slabs;
+        p->lds_bytes = 2 * AG_SLOT + sizeof(TileSide) + 2 * AG_REQS * 4;
+        p->bytes = p->off_part + up256((size_t)p->n_part * N * 4);
+        return true;
+    }
     const size_t group = (size_t)p->nks * ks * (dtype == AT_F32 ? 4 : 2) * 16 + 16 * sizeof(Side);
     int ng = B <= 16 ? 1 : B <= 32 ? 2 : 4;
     while (ng > 1 && group * ng > (size_t)AT_LDS)
@@ -1162,8 +1466,7 @@ bool plan_usage(int B, int N, int d, int dtype, int n_cu, UsagePlan *p)
     p->n_qt = (B + ng * 16 - 1) / (ng * 16);
     shares(p->slabs, slab, dtype, d, p->n_qt, n_cu, &p->n_chunks, &p->waves);
     p->lds_bytes = group * ng;
-    p->off_side = 0;
-    p->off_part = up256((size_t)B * sizeof(Side));
+    p->n_part = p->n_qt;
     p->bytes = p->off_part + (p->n_qt > 1 ? up256((size_t)p->n_qt * N * 4) : 0);
     return true;
 }
@@ -1190,14 +1493,15 @@ hipError_t launch_usage(const UsagePlan &p, const AttendBank &b, const float *ls
     a.slabs = p.slabs;
     a.decay = decay;
     a.usage = usage;
-    a.part = p.n_qt > 1 ? (float *)((uint8_t *)ws + p.off_part) : nullptr;
-    e = p.dtype == AT_F32    ? usage_dt<AT_F32>(p, a, s)
+    a.part = p.gemm || p.n_part > 1 ? (float *)((uint8_t *)ws + p.off_part) : nullptr;
+    e = p.gemm               ? usage_gemm(p, a, s)
+        : p.dtype == AT_F32  ? usage_dt<AT_F32>(p, a, s)
         : p.dtype == AT_BF16 ? usage_dt<AT_BF16>(p, a, s)
                              : usage_dt<AT_Q4>(p, a, s);
-    if (e != hipSuccess || p.n_qt == 1)
+    if (e != hipSuccess || !a.part)
         return e;
-    hipLaunchKernelGGL(usage_join_kernel, dim3((unsigned)(((long)b.N + 255) / 256)), dim3(256), 0, s, a.part, p.n_qt,
-                       b.N, decay, usage);
+    hipLaunchKernelGGL(usage_join_kernel, dim3((unsigned)(((long)b.N + 255) / 256)), dim3(256), 0, s, a.part,
+                       p.n_part, b.N, decay, usage);
     return hipGetLastError();
 }
 
@@ -1227,10 +1531,11 @@ bool plan_grad(int B, int N, int d, int dtype, int M, int n_cu, GradPlan *p)
     p->pitch = (2 * M + 15) / 16 * 16 + 4;
     const size_t group = (size_t)p->nks * ks * (dtype == AT_F32 ? 4 : 2) * 16 + 16 * sizeof(Side);
     const size_t tab = (size_t)p->pitch * 4 * 16;
+    p->gemm = at_gemm(dtype, B, N, d) && 2 * M <= 16;
     int ng = B <= 16 ? 1 : B <= 32 ? 2 : 4;
-    while (ng > 1 && group * ng > (size_t)AT_LDS)
+    while (ng > 1 && !p->gemm && group * ng > (size_t)AT_LDS)
         ng /= 2;
-    if (group * ng > (size_t)AT_LDS)
+    if (!p->gemm && group * ng > (size_t)AT_LDS)
         return false;
     p->tab = (group + tab) * ng <= (size_t)AT_LDS;
     p->ng = ng;
@@ -1246,8 +1551,18 @@ bool plan_grad(int B, int N, int d, int dtype, int M, int n_cu, GradPlan *p)
         part = p->slabs;
     const int n_parts = (int)((p->slabs + part - 1) / part);
     part = (p->slabs + n_parts - 1) / n_parts;
+    if (p->gemm)   // (whole tiles)
+        part = (part + 7) / 8 * 8;
     p->part_slabs = (int)part;
-    shares((int)part, AT_SLAB, dtype, d, p->n_qt, n_cu, &p->n_chunks, &p->waves);
+    p->n_gt = (B + ag_reqs(DS_RT) - 1) / ag_reqs(DS_RT);
+    if (p->gemm) {
+        p->nks = (d + AG_K - 1) / AG_K;
+        const long most = n_cu / p->n_gt, tiles256 = part / 8;
+        p->n_chunks = (int)(most < 1 ? 1 : most < tiles256 ? most : tiles256);
+        p->waves = AT_WAVES;
+    } else {
+        shares((int)part, AT_SLAB, dtype, d, p->n_qt, n_cu, &p->n_chunks, &p->waves);
+    }
     const long tiles = (long)((d + DQ_COLS - 1) / DQ_COLS) *
                        ((B + DQ_GROUPS * 16 - 1) / (DQ_GROUPS * 16));
     long qc = n_cu / tiles;
@@ -1258,7 +1573,9 @@ bool plan_grad(int B, int N, int d, int dtype, int M, int n_cu, GradPlan *p)
     p->q_chunks = (int)(qc > part ? part : qc);
     const size_t lds = (group + (p->tab ? tab : 0)) * ng;
     const size_t join = (size_t)p->waves * ng * 16 * 2 * 4;
-    p->lds_bytes = lds > join ? lds : join;
+    p->lds_bytes = p->gemm ? 2 * ag_slot(DS_RT) + sizeof(TileSide) + 3 * ag_reqs(DS_RT) * 4 +
+                                 (ag_reqs(DS_RT) / 16 + 16) * 4 * WAVE * 4
+                   : lds > join ? lds : join;
     const int n_dt = (d + 31) / 32 * 2;
     p->n_dt = n_dt;
     if ((size_t)p->n_blk * n_dt * WAVE * 16 >= (size_t)1 << 31)   // (32-bit offsets)
