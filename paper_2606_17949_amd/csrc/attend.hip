@@ -554,7 +554,7 @@ bool plan_attend(int B, int N, int d, int dtype, int M, int n_cu, AttendPlan *p)
     const int ks = at_ks(dtype);
     p->dtype = dtype;
     p->nks = (d + ks - 1) / ks;
-    p->gemm = at_gemm(dtype, B, N, d);
+    p->gemm = at_gemm(dtype, B, N, d, AG_REQS, n_cu);
     if (p->gemm) {
         p->nks = (d + AG_K - 1) / AG_K;
         p->ct = 1;
@@ -574,10 +574,8 @@ bool plan_attend(int B, int N, int d, int dtype, int M, int n_cu, AttendPlan *p)
     p->ct = 2 * M <= 16 ? 1 : 2;
     p->n_lt = (2 * M + 16 * p->ct - 1) / (16 * p->ct);
     const size_t group = (size_t)p->nks * ks * (dtype == AT_F32 ? 4 : 2) * 16;
-    int ng = B <= 16 ? 1 : B <= 32 ? 2 : 4;
-    while (ng > 1 && group * ng > (size_t)AT_LDS)
-        ng /= 2;
-    if (group * ng > (size_t)AT_LDS)
+    const int ng = at_groups(B, N, group, n_cu, 1, [&](int g) { return 16 * at_rt(dtype, g); });
+    if (ng == 0)
         return false;
     p->ng = ng;
     const int slab = 16 * at_rt(dtype, ng);

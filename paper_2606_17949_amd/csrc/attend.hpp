@@ -39,10 +39,35 @@ struct AttendPlan {
     size_t off_ml, off_o, bytes;   // workspace: partial maxima and sums, partial averages
 };
 
-// Whether a batch goes by as a matrix product of tiles (attend_gemm.hpp).
-inline bool at_gemm(int dtype, int B, int, int d)
+// Whether a batch goes by as a matrix product of tiles (attend_gemm.hpp) of 256
+// rows and `reqs` requests: more than half a tile of bf16 requests, of which
+// tiles for half the compute units, so that the scan by tiles of 64 would read
+// the bank three times or more. Forward, scan / tiles: 256 x 100,000 x 768 97 /
+// 67 us, 512 x 100,000 x 384 95 / 83, but 128 x 100,000 x 768 59 / 67 and 150 x
+// 15,000 x 768 30 / 40.
+inline bool at_gemm(int dtype, int B, int N, int d, int reqs, int n_cu)
 {
-    return dtype == AT_BF16 && B > 64 && d >= 128;
+    const long tiles = ((long)N + 255) / 256 * ((B + reqs - 1) / reqs);
+    return dtype == 1 && d >= 128 && B > reqs / 2 && 2 * tiles >= n_cu;
+}
+
+// Groups of 16 requests of a scan's tile: four where LDS holds them, fewer for a
+// smaller batch, and fewer for a small bank, so that two waves a compute unit
+// have something to do (64 x 1,000 x 768: 31 us by one tile of 64, 19 by four of
+// 16), but at least `least`. `group`: bytes of LDS of 16 requests; slab(ng): rows
+// of a slab. 0: none fits.
+template <typename Slab>
+int at_groups(int B, int N, size_t group, int n_cu, int least, Slab slab)
+{
+    int ng = B <= 16 ? 1 : B <= 32 ? 2 : 4;
+    while (ng > 1 && group * ng > (size_t)AT_LDS)
+        ng /= 2;
+    if (group * ng > (size_t)AT_LDS)
+        return 0;
+    while (ng > least && ((long)N + slab(ng) - 1) / slab(ng) * ((B + 16L * ng - 1) / (16 * ng)) <
+                         2L * n_cu)
+        ng /= 2;
+    return ng;
 }
 
 // The forward pass on a device of n_cu compute units; false if no layout fits.

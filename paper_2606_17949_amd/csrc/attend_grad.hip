@@ -941,7 +941,7 @@ __global__ __launch_bounds__(512, 1) void dx_kernel(const DxArgs A)
         const size_t row = (size_t)(A.row0 + lr);
         const bool live = !A.mask || A.mask[row] != 0;
         // (eight columns a lane: 16 rows x 64 bytes an instruction of bf16; four at a
-        // time took 160 us for FIXDX at 256 x 100,000 x 768)
+        // time took 160 us for 131 at 256 x 100,000 x 768)
 #pragma unroll
         for (int k = 0; k < NC; k += 2) {
             const int c0 = dealt_column(dt0 + k, 4 * jg);
@@ -1440,7 +1440,7 @@ bool plan_usage(int B, int N, int d, int dtype, int n_cu, UsagePlan *p)
     const int ks = at_ks(dtype);
     p->dtype = dtype;
     p->nks = (d + ks - 1) / ks;
-    p->gemm = at_gemm(dtype, B, N, d);
+    p->gemm = at_gemm(dtype, B, N, d, AG_REQS, n_cu);
     p->off_side = 0;
     p->off_part = up256((size_t)B * sizeof(Side));
     if (p->gemm) {
@@ -1455,10 +1455,8 @@ bool plan_usage(int B, int N, int d, int dtype, int n_cu, UsagePlan *p)
         return true;
     }
     const size_t group = (size_t)p->nks * ks * (dtype == AT_F32 ? 4 : 2) * 16 + 16 * sizeof(Side);
-    int ng = B <= 16 ? 1 : B <= 32 ? 2 : 4;
-    while (ng > 1 && group * ng > (size_t)AT_LDS)
-        ng /= 2;
-    if (group * ng > (size_t)AT_LDS)
+    const int ng = at_groups(B, N, group, n_cu, 1, [&](int g) { return 16 * at_rt(dtype, g); });
+    if (ng == 0)
         return false;
     p->ng = ng;
     const int slab = 16 * at_rt(dtype, ng);
@@ -1531,11 +1529,13 @@ bool plan_grad(int B, int N, int d, int dtype, int M, int n_cu, GradPlan *p)
     p->pitch = (2 * M + 15) / 16 * 16 + 4;
     const size_t group = (size_t)p->nks * ks * (dtype == AT_F32 ? 4 : 2) * 16 + 16 * sizeof(Side);
     const size_t tab = (size_t)p->pitch * 4 * 16;
-    p->gemm = at_gemm(dtype, B, N, d) && 2 * M <= 16;
-    int ng = B <= 16 ? 1 : B <= 32 ? 2 : 4;
-    while (ng > 1 && !p->gemm && group * ng > (size_t)AT_LDS)
-        ng /= 2;
-    if (!p->gemm && group * ng > (size_t)AT_LDS)
+    p->gemm = at_gemm(dtype, B, N, d, ag_reqs(DS_RT), n_cu) && 2 * M <= 16;
+    // (a wave of the tiled pass has 64 requests; a bf16 fragment of ds is of two
+    // groups, which one tile has to hold where there are two)
+    const int least = dtype == AT_BF16 && B > 16 ? 2 : 1;
+    const int ng =
+        p->gemm ? 4 : at_groups(B, N, group, n_cu, least, [](int) { return AT_SLAB; });
+    if (ng < least)
         return false;
     p->tab = (group + tab) * ng <= (size_t)AT_LDS;
     p->ng = ng;
@@ -1568,8 +1568,8 @@ bool plan_grad(int B, int N, int d, int dtype, int M, int n_cu, GradPlan *p)
     long qc = n_cu / tiles;
     qc = qc < 1 ? 1 : qc;
     // (a share's masks are kept in LDS)
-    const long least = (part + DQ_MASKS - 1) / DQ_MASKS;
-    qc = qc < least ? least : qc;
+    const long fewest = (part + DQ_MASKS - 1) / DQ_MASKS;
+    qc = qc < fewest ? fewest : qc;
     p->q_chunks = (int)(qc > part ? part : qc);
     const size_t lds = (group + (p->tab ? tab : 0)) * ng;
     const size_t join = (size_t)p->waves * ng * 16 * 2 * 4;

@@ -80,6 +80,11 @@ SIZES = [
     (64, 5001, (768, 768, 768), 4, 8.0), (65, 3000, (132, 136, 128), 5, 50.0),
     (130, 700, (516, 1000, 1024), 33, 3.0), (70, 1300, (2048, 2048, 2048), 4, 8.0),
     (200, 20_011, (96, 128, 128), 2, 6.0),
+    # bf16 batches that go by as products of tiles of 256 rows: one and more
+    # tiles of 256 and of 128 requests, rows that end inside a stage, 16 label
+    # columns and more
+    (129, 33_000, (16, 136, 160), 8, 10.0), (300, 20_011, (24, 200, 128), 5, 5.0),
+    (513, 11_009, (32, 128, 192), 9, 20.0), (100, 33_025, (8, 264, 32), 3, 12.0),
 ]
 
 
