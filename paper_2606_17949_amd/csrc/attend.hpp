@@ -106,7 +106,7 @@ struct GradPlan {
     bool tab;             // the label gradients of a request tile fit LDS
     int n_blk;            // blocks of requests of one fragment of ds (32, fp32 16)
     int n_dt;             // fragments of 16 columns of a block of requests
-    int pitch;            // floats of a request's label gradients
+    int n_j;              // pieces of 4 label columns, a multiple of four
     int part_slabs;       // slabs of a part
     int q_chunks;         // shares of a part in the d_queries pass
     size_t lds_bytes;

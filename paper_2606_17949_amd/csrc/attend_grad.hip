@@ -27,17 +27,31 @@ struct Side {
 
 struct PrepArgs {
     const uint8_t *queries;
-    int B, d, M, pitch;
+    int B, d, M, n_j;
     const float *lse, *q_hat, *l_hat, *dq, *dl, *dlse;
-    float *dout;     // [B][pitch] label gradients, 0 past 2 M; null: not wanted
+    float *dout;     // label gradients as fragments (dout_place); null: not wanted
     Side *side;
     int n_blk, n_dt; // fragments of the requests, [n_blk][n_dt][64]
     i32x4 *qpack;
 };
 
+// The label gradients as MFMA fragments, [group of 16 requests][n_j][64]: column
+// c of request b, lane (request % 16, column % 4) of piece c/4. n_j: pieces, a
+// multiple of four; columns past the labels and requests past the batch hold 0.
+__device__ __forceinline__ size_t dout_place(int b, int c, int n_j)
+{
+    return ((size_t)(b >> 4) * n_j + (c >> 2)) * WAVE + (c & 3) * 16 + (b & 15);
+}
+
 template <int QDT>
 __device__ __forceinline__ void make_side(const PrepArgs &A, int b, int lane)
 {
+    if (b >= A.B) {   // (places of the last group)
+        if (A.dout && b < (A.B + 15) / 16 * 16)
+            for (int c = lane; c < 4 * A.n_j; c += WAVE)
+                A.dout[dout_place(b, c, A.n_j)] = 0.f;
+        return;
+    }
     const int n16 = A.d * Elem<QDT>::ESZ / 16;
     const uint8_t *q = A.queries + (size_t)b * A.d * Elem<QDT>::ESZ;
     float s = 0.f;
@@ -49,7 +63,7 @@ __device__ __forceinline__ void make_side(const PrepArgs &A, int b, int lane)
     float dot = 0.f;
     if (A.dout) {
         // (a dead request's outputs are no numbers, and its gradients may be none)
-        for (int c = lane; c < A.pitch; c += WAVE) {
+        for (int c = lane; c < 4 * A.n_j; c += WAVE) {
             float g = 0.f, o = 0.f;
             if (alive && c < 2 * A.M) {
                 const size_t at = (size_t)b * A.M + (c < A.M ? c : c - A.M);
@@ -57,7 +71,7 @@ __device__ __forceinline__ void make_side(const PrepArgs &A, int b, int lane)
                 o = c < A.M ? A.q_hat[at] : A.l_hat[at];
             }
             dot = fmaf(g, o, dot);
-            A.dout[(size_t)b * A.pitch + c] = g;
+            A.dout[dout_place(b, c, A.n_j)] = g;
         }
         dot = wave_sum(dot);
         if (alive && A.dlse)
@@ -115,9 +129,7 @@ template <int QDT>
 __global__ __launch_bounds__(256) void prep_kernel(const PrepArgs A, int side_blocks)
 {
     if ((int)blockIdx.x < side_blocks) {
-        const int b = blockIdx.x * 4 + (threadIdx.x >> 6);
-        if (b < A.B)
-            make_side<QDT>(A, b, threadIdx.x & 63);
+        make_side<QDT>(A, blockIdx.x * 4 + (threadIdx.x >> 6), threadIdx.x & 63);
     } else {
         make_qpack<QDT>(A, (long)(blockIdx.x - side_blocks) * 256 + threadIdx.x);
     }
@@ -301,8 +313,8 @@ struct DsArgs {
     const float *qual, *len;
     int M;
     const Side *side;
-    const float *dout;      // [B][pitch]
-    int pitch;
+    const float *dout;      // fragments, n_j pieces a group
+    int n_j;
     int nks, n_chunks, n_qt, n_blk;
     long slab0, slabs;      // this part
     i32x4 *ds;              // of this part, null if neither product is wanted
@@ -323,19 +335,202 @@ __device__ __forceinline__ int ds_place(int lane)
     return (lane & 48) | ((lane & 15) ^ ((lane >> 4) << 2));
 }
 
-// ds of a part: p from the recomputed scores, dp = dout . labels by fp32 MFMA,
-// ds = p * (dp - shift). It goes out as MFMA fragments of the products that
-// follow: bf16 banks as two bf16 values, hi + lo = ds to 2^-17 (one value
-// alone, 2^-9, would add as much error to the gradients as their own rounding
-// does); fp32 banks as it is. With the bank's rows over the lanes, p is also
-// the operand of the labels' gradient p^T . dout as it stands.
+// A wave's 16 rows of the bank in the passes below; the same for all its lanes.
+struct RowTile {
+    long row0, tile16;   // first row, number among the part's row tiles
+    int rows;            // rows of the bank in it
+    int t, q0;           // request tile (of rowsum and the labels' gradients), its first request
+};
+
+// ds of 16 rows and NG groups of requests: p from the recomputed scores, dp =
+// dout . labels by fp32 MFMA, ds = p * (dp - shift). It goes out as MFMA fragments
+// of the products that follow: bf16 banks as two bf16 values, hi + lo = ds to
+// 2^-17 (one value alone, 2^-9, would add as much error to the gradients as their
+// own rounding does); fp32 banks as it is. With the bank's rows over the lanes, p
+// is also the operand of the labels' gradient p^T . dout as it stands.
+//   sd     [3][stride] in LDS: hq, lse2, shift of these requests
+//   tab    label gradients of these requests, fragments of n_j pieces
+//   sc     <q, x> of row l%16 and requests 16*g + 4*(l/16) + e
+//   lab(c) the lane's label, of column c + l/16 in row l%16
+template <int DT, int NG, typename Lab>
+__device__ __forceinline__ void ds_row_tile(const DsArgs &A, const RowTile &T, const float *sd,
+                                            int stride, const float *tab, int l, float nh,
+                                            f32x4 (&sc)[NG], Lab &&lab, float (&sum_ds)[NG][4],
+                                            float (&sum_db)[NG][4])
+{
+    const int col = l & 15, jg = l >> 4, M = A.M;
+    const float c = A.b.c;
+    const bool live = nh != -INFINITY;
+    auto side4 = [&](int which, int g) {
+        return *(const f32x4 *)(sd + which * stride + 16 * g + 4 * jg);
+    };
+    // (what the requests have in LDS is read again for every row tile: kept in
+    // registers it would not leave room for the scores)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4 dp[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+        dp[g] = -side4(2, g);
+    auto dp_step = [&](int j) {
+        // (a masked row's labels may be no numbers)
+        const float x = live && 4 * j + jg < 2 * M ? lab(j) : 0.f;
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+            dp[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(tab[(g * A.n_j + j) * WAVE + l], x, dp[g],
+                                                         0, 0, 0);
+    };
+    static_for<0, 4>([&](auto J) {
+        if (4 * decltype(J)::value < 2 * M)
+            dp_step(decltype(J)::value);
+    });
+    for (int j = 4; 4 * j < 2 * M; ++j)
+        dp_step(j);
+    // ---- p in place of the scores, ds in place of dp
+    float rs = 0.f;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        __builtin_amdgcn_sched_barrier(0);
+        const f32x4 hq = side4(0, g), lse2 = side4(1, g);
+        float ds[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float a = live ? sc[g][e] + (nh + hq[e]) : 0.f;
+            const float p = live ? __builtin_amdgcn_exp2f(fmaf(c, a, -lse2[e])) : 0.f;
+            ds[e] = p * dp[g][e];
+            sc[g][e] = p;
+            sum_db[g][e] = fmaf(2.f * a, ds[e], sum_db[g][e]);   // -distance = 2 a
+        }
+        if constexpr (DT == AT_BF16) {
+            int h[2], w[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float y0 = ds[2 * i], y1 = ds[2 * i + 1];
+                h[i] = split_bf16(y0, y1);
+                w[i] = split_bf16(y0, y1);
+                ds[2 * i] -= y0;       // what the two values hold
+                ds[2 * i + 1] -= y1;
+            }
+            dp[g] = __builtin_bit_cast(f32x4, i32x4{h[0], h[1], w[0], w[1]});
+        } else {
+            dp[g] = f32x4{ds[0], ds[1], ds[2], ds[3]};
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            sum_ds[g][e] += ds[e];
+            rs += ds[e];
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    const bool any = T.q0 < A.b.B;
+    // ---- fragments of ds: [row tile][block of requests][hi, lo][64]
+    if (A.ds) {
+        constexpr int H = DT == AT_BF16 ? 2 : 1;   // values, and groups of a block
+        const uint32_t place = (uint32_t)ds_place(l) * 16;
+#pragma unroll
+        for (int g = 0; g < NG; g += H) {
+            const int blk = T.q0 / (16 * H) + g / H;
+            const __amdgpu_buffer_rsrc_t to =
+                wave_rsrc(A.ds + (T.tile16 * A.n_blk + min(blk, A.n_blk - 1)) * H * WAVE,
+                          blk < A.n_blk ? H * WAVE * 16u : 0u);
+            if constexpr (H == 2) {
+                const f32x4 none = f32x4{0.f, 0.f, 0.f, 0.f};
+                const f32x4 x = dp[g], y = g + 1 < NG ? dp[g + 1 < NG ? g + 1 : g] : none;
+                const bool turned = col & 4;
+                const f32x4 u = turned ? y : x, w = turned ? x : y;
+                __builtin_amdgcn_raw_buffer_store_b128(
+                    __builtin_bit_cast(i32x4, f32x4{u[0], u[1], w[0], w[1]}), to, (int)place, 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b128(
+                    __builtin_bit_cast(i32x4, f32x4{u[2], u[3], w[2], w[3]}), to,
+                    (int)(place + WAVE * 16), 0, 0);
+            } else {
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, dp[g]), to,
+                                                       (int)place, 0, 0);
+            }
+        }
+        rs = rows_reduce(rs, [](float x, float y) { return x + y; });
+        buffer_store4(wave_rsrc(A.rowsum + (any ? (size_t)T.t * A.part_rows : 0) + T.tile16 * 16,
+                                any ? 64u : 0u),
+                      jg == 0 ? (uint32_t)col * 4u : OFF_NONE, rs);
+    }
+    // ---- the labels' gradient: 16 columns x 16 rows, 4 requests a step
+    if (A.d_qual || A.d_len) {
+        const size_t at = ((size_t)(any ? T.t : 0) * A.b.N + T.row0) * M;
+        const uint32_t bytes = any ? (uint32_t)(T.rows * M) * 4u : 0u;
+        const __amdgpu_buffer_rsrc_t to_q =
+            wave_rsrc((A.d_qual ? A.d_qual : A.d_len) + at, A.d_qual ? bytes : 0u);
+        const __amdgpu_buffer_rsrc_t to_l =
+            wave_rsrc((A.d_len ? A.d_len : A.d_qual) + at, A.d_len ? bytes : 0u);
+        for (int k = 0; 16 * k < 2 * M; ++k) {
+            f32x4 dv = f32x4{0.f, 0.f, 0.f, 0.f};
+            const int cl = 16 * k + col;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                // of label column cl, this lane's four requests
+                const f32x4 d4 = *(const f32x4 *)(tab + (g * A.n_j + (cl >> 2)) * WAVE +
+                                                  (cl & 3) * 16 + 4 * jg);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    dv = __builtin_amdgcn_mfma_f32_16x16x4f32(d4[e], sc[g][e], dv, 0, 0, 0);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int cc = 16 * k + 4 * jg + e;
+                const uint32_t to = (uint32_t)(col * M + cc) * 4u;
+                buffer_store4(to_q, cc < M ? to : OFF_NONE, dv[e]);
+                buffer_store4(to_l, cc >= M && cc < 2 * M ? to - 4u * M : OFF_NONE, dv[e]);
+            }
+        }
+    }
+}
+
+// A wave's sums over its rows, [NG][4] of the lane, to places at[request][2].
+template <int NG>
+__device__ __forceinline__ void put_sums(const float (&sum_ds)[NG][4],
+                                         const float (&sum_db)[NG][4], float *at, int lane)
+{
+    auto add = [](float x, float y) { return x + y; };
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float x = row16_reduce(sum_ds[g][e], add), y = row16_reduce(sum_db[g][e], add);
+            if ((lane & 15) == 0) {
+                float *to = at + (16 * g + 4 * (lane >> 4) + e) * 2;
+                to[0] = x;
+                to[1] = y;
+            }
+        }
+}
+
+// The side data of n requests from q0 on into LDS, [3][n].
+__device__ __forceinline__ void load_side(const DsArgs &A, int q0, int n, float *sd)
+{
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const Side x = q0 + i < A.b.B ? A.side[q0 + i] : Side{0.f, INFINITY, 0.f, 0.f};
+        sd[i] = x.hq;
+        sd[n + i] = x.lse2;
+        sd[2 * n + i] = x.shift;
+    }
+}
+
+// The label gradients of n requests (whole groups) from q0 on into LDS.
+__device__ __forceinline__ void load_dout(const DsArgs &A, int q0, int n, float *tab)
+{
+    const int groups = (A.b.B + 15) / 16 - q0 / 16, per = A.n_j * WAVE;
+    for (int i = threadIdx.x; i < n / 16 * per; i += blockDim.x)
+        tab[i] = i < groups * per ? A.dout[(size_t)(q0 / 16) * per + i] : 0.f;
+}
+
+// The pass by tiles of NG * 16 requests, as the forward one. TAB: their label
+// gradients are in LDS.
 template <int DT, int NG, bool TAB>
 __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_kernel(const DsArgs A)
 {
     extern __shared__ __align__(16) uint8_t smem[];
     i32x4 *qs = (i32x4 *)smem;
     float *sd = (float *)(qs + (size_t)A.nks * NG * WAVE);   // [3][NG * 16] hq, lse2, shift
-    float *tab = sd + 4 * NG * 16;                           // [NG * 16][pitch]
+    float *tab = sd + 4 * NG * 16;                           // [NG][n_j][64]
     int t, ch;
     chunk_and_tile(A.n_chunks, A.n_qt, &ch, &t);
     if (ch >= A.n_chunks)
@@ -343,33 +538,14 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_kernel(const DsArgs A)
     const int tid = threadIdx.x, lane = tid & 63;
     const int n_waves = blockDim.x >> 6;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col = lane & 15, jg = lane >> 4;
     const int q0 = t * NG * 16;
     const long gw = (long)ch * n_waves + wave, n_gw = (long)A.n_chunks * n_waves;
     const long s0 = A.slab0 + gw * A.slabs / n_gw, s1 = A.slab0 + (gw + 1) * A.slabs / n_gw;
     const int N = A.b.N, M = A.M;
-    const float c = A.b.c;
     load_requests<DT, NG>(A.b, A.nks, q0, qs, wave, n_waves, lane);
-    for (int i = tid; i < NG * 16; i += blockDim.x) {
-        const Side x = q0 + i < A.b.B ? A.side[q0 + i] : Side{0.f, INFINITY, 0.f, 0.f};
-        sd[i] = x.hq;
-        sd[NG * 16 + i] = x.lse2;
-        sd[2 * NG * 16 + i] = x.shift;
-    }
-    // of this lane's four requests of group g
-    auto side4 = [&](int which, int g) {
-        return *(const f32x4 *)(sd + which * NG * 16 + g * 16 + 4 * jg);
-    };
+    load_side(A, q0, NG * 16, sd);
     if constexpr (TAB)
-        for (int i = tid; i < NG * 16 * A.pitch; i += blockDim.x)
-            tab[i] = q0 + i / A.pitch < A.b.B ? A.dout[(size_t)q0 * A.pitch + i] : 0.f;
-    // label gradient column cc of request q of the tile
-    auto dout = [&](int q, int cc) -> float {
-        if constexpr (TAB)
-            return tab[q * A.pitch + cc];
-        else
-            return A.dout[(size_t)min(q0 + q, A.b.B - 1) * A.pitch + cc];
-    };
+        load_dout(A, q0, NG * 16, tab);
     float sum_ds[NG][4], sum_db[NG][4];
 #pragma unroll
     for (int g = 0; g < NG; ++g)
@@ -380,14 +556,14 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_kernel(const DsArgs A)
     uint8_t mk[AT_RT];
     const bool masked = A.b.mask != nullptr;
     const uint8_t *const mask = masked ? A.b.mask : (const uint8_t *)A.b.norms;
-    const float *lab[4];   // label column 4*j + jg
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int cc = 4 * j + jg;
-        lab[j] = cc < M ? A.qual + cc : cc < 2 * M ? A.len + (cc - M) : A.qual;
-    }
+    auto column = [&](int l, int j, size_t row) {   // label 4*j + l/16 of a row, or another
+        const int cc = 4 * j + (l >> 4);
+        return (cc < M || cc >= 2 * M ? A.qual : A.len) + row * M +
+               (cc < M ? cc : cc < 2 * M ? cc - M : 0);
+    };
     auto side = [&](int slab) {
-        const long r0 = (s0 + slab) * AT_SLAB + col;
+        const int l = fresh(lane);
+        const long r0 = (s0 + slab) * AT_SLAB + (l & 15);
 #pragma unroll
         for (int r = 0; r < AT_RT; ++r) {
             const size_t at = (size_t)min(r0 + r * 16, (long)N - 1);
@@ -395,184 +571,34 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_kernel(const DsArgs A)
             mk[r] = mask[at];
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                vr[r][j] = lab[j][at * M];
+                vr[r][j] = *column(l, j, at);
         }
     };
-    const int n_ct = (2 * M + 15) / 16;
     auto end = [&](int slab, f32x4(&acc)[AT_RT][NG]) {
-        const long row0 = (s0 + slab) * AT_SLAB + col;
-        float nh[AT_RT];   // -inf for rows masked or past the bank
-#pragma unroll
-        for (int r = 0; r < AT_RT; ++r)
-            nh[r] = row0 + r * 16 < N && !(masked && mk[r] == 0) ? -0.5f * nrm[r] : -INFINITY;
-        // ---- dp: 4 label columns a step, request groups x row tiles
-        f32x4 dp[AT_RT][NG];
-#pragma unroll
-        for (int r = 0; r < AT_RT; ++r)
-#pragma unroll
-            for (int g = 0; g < NG; ++g)
-                dp[r][g] = -side4(2, g);
-        // (a masked row's labels may be no numbers)
-        auto dp_step = [&](int c0, float(&x)[AT_RT]) {
-            const int cc = c0 + jg;
-#pragma unroll
-            for (int r = 0; r < AT_RT; ++r)
-                x[r] = nh[r] != -INFINITY && cc < 2 * M ? x[r] : 0.f;
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                const float a = dout(g * 16 + col, cc);
-#pragma unroll
-                for (int r = 0; r < AT_RT; ++r)
-                    dp[r][g] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, x[r], dp[r][g], 0, 0, 0);
-            }
-        };
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (4 * j < 2 * M) {
-                float x[AT_RT];
-#pragma unroll
-                for (int r = 0; r < AT_RT; ++r)
-                    x[r] = vr[r][j];
-                dp_step(4 * j, x);
-            }
-        for (int c0 = 16; c0 < 2 * M; c0 += 4) {
-            const int cc = c0 + jg;
-            float x[AT_RT];
-#pragma unroll
-            for (int r = 0; r < AT_RT; ++r) {
-                const size_t at = (size_t)min(row0 + r * 16, (long)N - 1) * M;
-                x[r] = cc < M ? A.qual[at + cc] : cc < 2 * M ? A.len[at + cc - M] : 0.f;
-            }
-            dp_step(c0, x);
-        }
-        // ---- p in place of the scores, ds in place of dp
-        float rs[AT_RT];
+        const int l = fresh(lane);
 #pragma unroll
         for (int r = 0; r < AT_RT; ++r) {
-            rs[r] = 0.f;
-            const bool live = nh[r] != -INFINITY;
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                __builtin_amdgcn_sched_barrier(0);
-                const f32x4 hq = side4(0, g), lse2 = side4(1, g);
-                float hi[4], lo[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float a = live ? acc[r][g][e] + (nh[r] + hq[e]) : 0.f;
-                    const float p =
-                        live ? __builtin_amdgcn_exp2f(fmaf(c, a, -lse2[e])) : 0.f;
-                    const float ds = p * dp[r][g][e];
-                    acc[r][g][e] = p;
-                    sum_db[g][e] = fmaf(2.f * a, ds, sum_db[g][e]);   // -distance = 2 a
-                    float held = ds;
-                    if constexpr (DT == AT_BF16) {
-                        hi[e] = (float)(__bf16)ds;
-                        lo[e] = (float)(__bf16)(ds - hi[e]);
-                        held = hi[e] + lo[e];
-                    }
-                    dp[r][g][e] = ds;
-                    sum_ds[g][e] += held;
-                    rs[r] += held;
-                }
-                if constexpr (DT == AT_BF16) {
-                    // two bf16 to a register: hi in dp's first two, lo in its last two
-                    auto two = [](float x, float y) {
-                        return __uint_as_float((__float_as_uint(y) & 0xffff0000u) |
-                                               (__float_as_uint(x) >> 16));
-                    };
-                    dp[r][g] = f32x4{two(hi[0], hi[1]), two(hi[2], hi[3]), two(lo[0], lo[1]),
-                                     two(lo[2], lo[3])};
-                }
-            }
-        }
-        // ---- fragments of ds: [row tile][block of requests][hi, lo][64]
-        if (A.ds) {
-            const long tile0 = (s0 + slab - A.slab0) * AT_RT;
-            const int place = ds_place(lane);
-#pragma unroll
-            for (int r = 0; r < AT_RT; ++r) {
-                if constexpr (DT == AT_BF16) {
-#pragma unroll
-                    for (int g = 0; g < NG; g += 2) {
-                        const int blk = (q0 >> 5) + (g >> 1);
-                        if (blk >= A.n_blk)
-                            break;
-                        const f32x4 x = dp[r][g];
-                        f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
-                        if (g + 1 < NG)
-                            y = dp[r][g + 1 < NG ? g + 1 : g];
-                        i32x4 *at = A.ds + ((tile0 + r) * A.n_blk + blk) * 2 * WAVE + place;
-                        const bool turned = col & 4;
-                        const f32x4 u = turned ? y : x, v = turned ? x : y;
-                        at[0] = __builtin_bit_cast(i32x4, f32x4{u[0], u[1], v[0], v[1]});
-                        at[WAVE] = __builtin_bit_cast(i32x4, f32x4{u[2], u[3], v[2], v[3]});
-                    }
-                } else {
-#pragma unroll
-                    for (int g = 0; g < NG; ++g) {
-                        const int blk = (q0 >> 4) + g;
-                        if (blk < A.n_blk)
-                            A.ds[((tile0 + r) * A.n_blk + blk) * WAVE + place] =
-                                __builtin_bit_cast(i32x4, dp[r][g]);
-                    }
-                }
-                const float sum = rows_reduce(rs[r], [](float x, float y) { return x + y; });
-                if (jg == 0)
-                    A.rowsum[(size_t)t * A.part_rows + (tile0 + r) * 16 + col] = sum;
-            }
-        }
-        // ---- the labels' gradient: 16 columns x 16 rows, 4 requests a step
-        if (A.d_qual || A.d_len) {
-            for (int k = 0; k < n_ct; ++k) {
-                f32x4 dv[AT_RT];
-#pragma unroll
-                for (int r = 0; r < AT_RT; ++r)
-                    dv[r] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int g = 0; g < NG; ++g)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float a = dout(g * 16 + 4 * jg + e, k * 16 + col);
-#pragma unroll
-                        for (int r = 0; r < AT_RT; ++r)
-                            dv[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, acc[r][g][e], dv[r],
-                                                                         0, 0, 0);
-                    }
-#pragma unroll
-                for (int r = 0; r < AT_RT; ++r) {
-                    const long row = row0 + r * 16;
-                    if (row < N)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int cc = k * 16 + 4 * jg + e;
-                            const size_t at = ((size_t)t * N + row) * M;
-                            if (cc < M) {
-                                if (A.d_qual)
-                                    A.d_qual[at + cc] = dv[r][e];
-                            } else if (cc < 2 * M && A.d_len)
-                                A.d_len[at + cc - M] = dv[r][e];
-                        }
-                }
-            }
+            const long row0 = (s0 + slab) * AT_SLAB + r * 16, row = row0 + (l & 15);
+            const float nh = row < N && !(masked && mk[r] == 0) ? -0.5f * nrm[r] : -INFINITY;
+            const RowTile T{row0, (s0 + slab - A.slab0) * AT_RT + r,
+                            (int)max(0L, min(16L, N - row0)), t, q0};
+            auto lab = [&](int j) {
+                return j < 4 ? (j == 0   ? vr[r][0]
+                                : j == 1 ? vr[r][1]
+                                : j == 2 ? vr[r][2]
+                                         : vr[r][3])
+                             : *column(l, j, (size_t)min(row, (long)N - 1));
+            };
+            const float *const douts = TAB ? tab : A.dout + (size_t)(q0 >> 4) * A.n_j * WAVE;
+            ds_row_tile<DT, NG>(A, T, sd, NG * 16, douts, l, nh, acc[r], lab, sum_ds, sum_db);
         }
     };
-    scan_slabs<DT, NG, AT_RT, at_ring(DT, AT_RT), true>(A.b, A.nks, qs, s0, s1, lane, [] {}, side, end);
-
+    scan_slabs<DT, NG, AT_RT, at_ring(DT, AT_RT), true>(A.b, A.nks, qs, s0, s1, lane, [] {}, side,
+                                                        end);
     // ---- the requests' sums, joined over the waves
     float *jn = (float *)smem;   // [n_waves][NG * 16][2]
     stream_barrier();
-#pragma unroll
-    for (int g = 0; g < NG; ++g)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            auto add = [](float x, float y) { return x + y; };
-            const float x = row16_reduce(sum_ds[g][e], add), y = row16_reduce(sum_db[g][e], add);
-            if (col == 0) {
-                float *at = jn + (wave * NG * 16 + g * 16 + 4 * jg + e) * 2;
-                at[0] = x;
-                at[1] = y;
-            }
-        }
+    put_sums<NG>(sum_ds, sum_db, jn + wave * NG * 32, lane);
     stream_barrier();
     for (int i = tid; i < NG * 32; i += blockDim.x) {
         if (q0 + i / 2 >= A.b.B)
@@ -586,10 +612,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_kernel(const DsArgs A)
 }
 
 // The same as a matrix product of tiles, for large bf16 batches and at most 16
-// label columns. Request tiles of 64 (a wave's) as above in rowsum and the
-// labels' gradients; the label gradients of the requests stand in LDS as the
-// fragments of dp, [groups][4][64], a tile's labels beside them, [16 row
-// tiles][4][64].
+// label columns; a tile's labels stand in LDS, [16 row tiles][4][64].
 constexpr int DS_RT = 4;
 
 __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_gemm_kernel(const DsArgs A)
@@ -599,7 +622,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_gemm_kernel(const DsArg
     TileSide *side = (TileSide *)(smem + 2 * ag_slot(DS_RT));
     float *sd = (float *)(side + 1);         // [3][REQS] hq, lse2, shift
     float *tab = sd + 3 * REQS;              // [REQS / 16][4][64]
-    float *labels = tab + REQS / 16 * 4 * WAVE;   // [16][4][64]
+    float *labels = tab + REQS / 16 * 4 * WAVE;
     int t, ch;
     chunk_and_tile(A.n_chunks, A.n_qt, &ch, &t);
     if (ch >= A.n_chunks)
@@ -607,25 +630,14 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_gemm_kernel(const DsArg
     const int tid = threadIdx.x, lane = tid & 63;
     __builtin_assume(tid < AT_WAVES * WAVE);
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col = lane & 15, jg = lane >> 4;
     const int wr = wave / WQ, wq = wave % WQ;
-    const int q0 = t * REQS, qw = q0 + 64 * wq, t64 = t * WQ + wq;
-    const bool any = qw < A.b.B;
+    const int q0 = t * REQS;
     const int n_tiles = (int)((A.slabs + 7) / 8);   // of the part
     const int t0 = (int)((long)ch * n_tiles / A.n_chunks),
               t1 = (int)((long)(ch + 1) * n_tiles / A.n_chunks);
     const int N = A.b.N, M = A.M;
-    const float c = A.b.c;
-    if (tid < REQS) {
-        const Side x = q0 + tid < A.b.B ? A.side[q0 + tid] : Side{0.f, INFINITY, 0.f, 0.f};
-        sd[tid] = x.hq;
-        sd[REQS + tid] = x.lse2;
-        sd[2 * REQS + tid] = x.shift;
-    }
-    for (int i = tid; i < REQS / 16 * 4 * WAVE; i += AT_WAVES * WAVE) {
-        const int q = q0 + (i >> 8) * 16 + (i & 15), cc = ((i >> 6) & 3) * 4 + ((i >> 4) & 3);
-        tab[i] = q < A.b.B ? A.dout[(size_t)q * A.pitch + cc] : 0.f;
-    }
+    load_side(A, q0, REQS, sd);
+    load_dout(A, q0, REQS, tab);
     const long part0 = A.slab0 * AT_SLAB;   // first row of the part
     float sum_ds[AG_NG][4], sum_db[AG_NG][4];
 #pragma unroll
@@ -634,7 +646,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_gemm_kernel(const DsArg
         for (int e = 0; e < 4; ++e)
             sum_ds[g][e] = sum_db[g][e] = 0.f;
     // the lane's address in piece 4*i + j of a tile's labels: row tile i, column
-    // 4*j + jg (behind the last column, the first again)
+    // 4*j + lane/16 (behind the last column, the first again)
     auto label = [&](long row0, int f, int l) {
         const long row = min(row0 + (f >> 2) * 16 + (l & 15), (long)N - 1);
         const int cc = 4 * (f & 3) + (l >> 4);
@@ -642,152 +654,33 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_gemm_kernel(const DsArg
                (cc < M ? cc : cc < 2 * M ? cc - M : 0);
     };
     auto end = [&](int tile, f32x4(&acc)[DS_RT][AG_NG]) {
-        const int l = fresh(lane), col = l & 15, jg = l >> 4;
-        // this lane's places in 16 rows of the labels' gradients (columns 4*jg + e of
-        // row col) and in a fragment of ds
-        uint32_t off_q[4], off_l[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int cc = 4 * jg + e;
-            off_q[e] = cc < M ? (uint32_t)(col * M + cc) * 4u : OFF_NONE;
-            off_l[e] = cc >= M && cc < 2 * M ? (uint32_t)(col * M + cc - M) * 4u : OFF_NONE;
-        }
-        const uint32_t place = (uint32_t)ds_place(l) * 16;
+        const int l = fresh(lane);
         const long row0 = part0 + (long)(t0 + tile) * AG_ROWS;
         const int left = (int)min((long)AG_ROWS, N - row0);
-        const long tile16 = (long)(t0 + tile) * 16 + DS_RT * wr;   // of the part's row tiles
-        const int r0 = 16 * DS_RT * wr;   // this wave's rows
-        const size_t lab_at = ((size_t)(any ? t64 : 0) * N + row0 + r0) * M;
 #pragma unroll
         for (int r = 0; r < DS_RT; ++r) {
-            // (what the requests have in LDS is read again for every row tile: kept
-            // in registers it would not leave room for the scores)
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_sched_barrier(0);
-            const float nh = tile_norm(A.b, side, left, r0 + 16 * r + col);
-            const bool live = nh != -INFINITY;
-            float x[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                x[j] = live && 4 * j + jg < 2 * M
-                           ? labels[((DS_RT * wr + r) * 4 + j) * WAVE + l]
-                           : 0.f;
-            f32x4 dp[AG_NG];
-#pragma unroll
-            for (int g = 0; g < AG_NG; ++g)
-                dp[g] = -*(const f32x4 *)(sd + 2 * REQS + 64 * wq + 16 * g + 4 * jg);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (4 * j < 2 * M)
-#pragma unroll
-                    for (int g = 0; g < AG_NG; ++g)
-                        dp[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                            tab[((4 * wq + g) * 4 + j) * WAVE + l], x[j], dp[g], 0, 0, 0);
-            float rs = 0.f;
-#pragma unroll
-            for (int g = 0; g < AG_NG; ++g) {
-                __builtin_amdgcn_sched_barrier(0);
-                const float *s4 = sd + 64 * wq + 16 * g + 4 * jg;
-                const f32x4 hq = *(const f32x4 *)s4, lse2 = *(const f32x4 *)(s4 + REQS);
-                float ds[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float a = live ? acc[r][g][e] + (nh + hq[e]) : 0.f;
-                    const float p = live ? __builtin_amdgcn_exp2f(fmaf(c, a, -lse2[e])) : 0.f;
-                    ds[e] = p * dp[g][e];
-                    acc[r][g][e] = p;
-                    sum_db[g][e] = fmaf(2.f * a, ds[e], sum_db[g][e]);   // -distance = 2 a
-                }
-                int h[2], l[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float y0 = ds[2 * i], y1 = ds[2 * i + 1];
-                    h[i] = split_bf16(y0, y1);
-                    l[i] = split_bf16(y0, y1);
-                    // what the two bf16 values hold: ds less what they leave
-                    const float z0 = ds[2 * i] - y0, z1 = ds[2 * i + 1] - y1;
-                    sum_ds[g][2 * i] += z0;
-                    sum_ds[g][2 * i + 1] += z1;
-                    rs += z0 + z1;
-                }
-                dp[g] = __builtin_bit_cast(f32x4, i32x4{h[0], h[1], l[0], l[1]});
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            if (A.ds) {
-#pragma unroll
-                for (int g = 0; g < AG_NG; g += 2) {
-                    const int blk = (qw >> 5) + (g >> 1);
-                    const __amdgpu_buffer_rsrc_t to =
-                        wave_rsrc(A.ds + ((tile16 + r) * A.n_blk + min(blk, A.n_blk - 1)) * 2 * WAVE,
-                                  blk < A.n_blk ? 2 * WAVE * 16u : 0u);
-                    const bool turned = col & 4;
-                    const f32x4 u = turned ? dp[g + 1] : dp[g], w = turned ? dp[g] : dp[g + 1];
-                    __builtin_amdgcn_raw_buffer_store_b128(
-                        __builtin_bit_cast(i32x4, f32x4{u[0], u[1], w[0], w[1]}), to, (int)place, 0,
-                        0);
-                    __builtin_amdgcn_raw_buffer_store_b128(
-                        __builtin_bit_cast(i32x4, f32x4{u[2], u[3], w[2], w[3]}), to,
-                        (int)(place + WAVE * 16), 0, 0);
-                }
-                rs = rows_reduce(rs, [](float y, float z) { return y + z; });
-                buffer_store4(wave_rsrc(A.rowsum + (any ? (size_t)t64 * A.part_rows : 0) +
-                                            (tile16 + r) * 16,
-                                        any ? 64u : 0u),
-                              jg == 0 ? (uint32_t)col * 4u : OFF_NONE, rs);
-            }
-            if (A.d_qual || A.d_len) {
-                f32x4 dv = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int g = 0; g < AG_NG; ++g) {
-                    // of label column `col`, this lane's four requests
-                    const f32x4 d4 = *(const f32x4 *)(tab + ((4 * wq + g) * 4 + (col >> 2)) * WAVE +
-                                                      (col & 3) * 16 + 4 * jg);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        dv = __builtin_amdgcn_mfma_f32_16x16x4f32(d4[e], acc[r][g][e], dv, 0, 0,
-                                                                  0);
-                }
-                const uint32_t rows = any ? (uint32_t)max(0, min(16, left - r0 - 16 * r)) : 0u;
-                const __amdgpu_buffer_rsrc_t to_q =
-                    wave_rsrc((A.d_qual ? A.d_qual : A.d_len) + lab_at + 16 * r * M,
-                              A.d_qual ? rows * M * 4u : 0u);
-                const __amdgpu_buffer_rsrc_t to_l =
-                    wave_rsrc((A.d_len ? A.d_len : A.d_qual) + lab_at + 16 * r * M,
-                              A.d_len ? rows * M * 4u : 0u);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    buffer_store4(to_q, off_q[e], dv[e]);
-                    buffer_store4(to_l, off_l[e], dv[e]);
-                }
-            }
+            const int r16 = DS_RT * wr + r;   // row tile of the tile
+            const float nh = tile_norm(A.b, side, left, 16 * r16 + (l & 15));
+            const RowTile T{row0 + 16 * r16, (long)(t0 + tile) * 16 + r16,
+                            max(0, min(16, left - 16 * r16)), t * WQ + wq, q0 + 64 * wq};
+            auto lab = [&](int j) { return labels[(r16 * 4 + j) * WAVE + l]; };
+            ds_row_tile<AT_BF16, AG_NG>(A, T, sd + 64 * wq, REQS, tab + 4 * wq * A.n_j * WAVE, l,
+                                        nh, acc[r], lab, sum_ds, sum_db);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
     gemm_tiles<DS_RT, true, 8>(A.b, A.nks, smem, side, labels, q0, A.slab0 / 8 + t0, t1 - t0, wave,
                                lane, label, end);
-
     // ---- the requests' sums, joined over the waves of a request
     float *jn = (float *)smem;   // [8 / WQ][REQS][2]
     stream_barrier();
-#pragma unroll
-    for (int g = 0; g < AG_NG; ++g)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            auto add = [](float x, float y) { return x + y; };
-            const float x = row16_reduce(sum_ds[g][e], add), y = row16_reduce(sum_db[g][e], add);
-            if (col == 0) {
-                float *to = jn + (wr * REQS + 64 * wq + 16 * g + 4 * jg + e) * 2;
-                to[0] = x;
-                to[1] = y;
-            }
-        }
+    put_sums<AG_NG>(sum_ds, sum_db, jn + (wr * REQS + 64 * wq) * 2, lane);
     stream_barrier();
-    const int i = tid;   // request i/2, sum i%2
-    if (i < 2 * REQS && q0 + i / 2 < A.b.B) {
+    if (tid < 2 * REQS && q0 + tid / 2 < A.b.B) {   // request tid/2, sum tid%2
         float s = 0.f;
         for (int w = 0; w < AT_WAVES / WQ; ++w)
-            s += jn[w * 2 * REQS + i];
-        float *to = A.req + ((size_t)ch * A.b.B + q0) * 2 + i;
+            s += jn[w * 2 * REQS + tid];
+        float *to = A.req + ((size_t)ch * A.b.B + q0) * 2 + tid;
         *to = A.first ? s : *to + s;
     }
 }
@@ -1329,7 +1222,7 @@ void shares(int slabs, int slab, int dtype, int d, int n_qt, int n_cu, int *n_ch
 template <int QDT>
 hipError_t run_prep(const PrepArgs &a, hipStream_t s)
 {
-    const int side_blocks = (a.B + 3) / 4;
+    const int side_blocks = (a.B + 15) / 16 * 4;   // (whole groups)
     const long frags = a.qpack ? (long)a.n_blk * a.n_dt * WAVE : 0;
     hipLaunchKernelGGL(prep_kernel<QDT>, dim3((unsigned)(side_blocks + (frags + 255) / 256)),
                        dim3(256), 0, s, a, side_blocks);
@@ -1353,7 +1246,7 @@ hipError_t run_grad(const GradPlan &p, const AttendBank &b, const GradArgs &g, u
     float *dout = (float *)(wb + p.off_dout);
     i32x4 *qpack = (i32x4 *)(wb + p.off_qpack);
     const int n_dt = p.n_dt;
-    hipError_t e = run_prep<QDT>({b.queries, b.B, b.d, g.M, p.pitch, g.lse, g.q_hat, g.l_hat,
+    hipError_t e = run_prep<QDT>({b.queries, b.B, b.d, g.M, p.n_j, g.lse, g.q_hat, g.l_hat,
                                   g.dq_hat, g.dl_hat, g.dlse, dout, side, p.n_blk, n_dt,
                                   g.d_bank ? qpack : nullptr},
                                  s);
@@ -1366,7 +1259,7 @@ hipError_t run_grad(const GradPlan &p, const AttendBank &b, const GradArgs &g, u
     a.M = g.M;
     a.side = side;
     a.dout = dout;
-    a.pitch = p.pitch;
+    a.n_j = p.n_j;
     a.nks = p.nks;
     a.n_chunks = p.n_chunks;
     a.n_qt = p.gemm ? p.n_gt : p.n_qt;
@@ -1526,9 +1419,9 @@ bool plan_grad(int B, int N, int d, int dtype, int M, int n_cu, GradPlan *p)
     p->dtype = dtype;
     p->nks = (d + ks - 1) / ks;
     p->slabs = (int)(((long)N + AT_SLAB - 1) / AT_SLAB);
-    p->pitch = (2 * M + 15) / 16 * 16 + 4;
+    p->n_j = (2 * M + 15) / 16 * 4;
     const size_t group = (size_t)p->nks * ks * (dtype == AT_F32 ? 4 : 2) * 16 + 16 * sizeof(Side);
-    const size_t tab = (size_t)p->pitch * 4 * 16;
+    const size_t tab = (size_t)p->n_j * WAVE * 4;
     p->gemm = at_gemm(dtype, B, N, d, ag_reqs(DS_RT), n_cu) && 2 * M <= 16;
     // (a wave of the tiled pass has 64 requests; a bf16 fragment of ds is of two
     // groups, which one tile has to hold where there are two)
@@ -1584,7 +1477,7 @@ bool plan_grad(int B, int N, int d, int dtype, int M, int n_cu, GradPlan *p)
     p->off_side = o;
     o += up256((size_t)B * sizeof(Side));
     p->off_dout = o;
-    o += up256((size_t)B * p->pitch * 4);
+    o += up256((size_t)((B + 15) / 16) * tab);
     p->off_qpack = o;
     o += up256((size_t)p->n_blk * n_dt * WAVE * 16);
     p->off_ds = o;
