@@ -356,7 +356,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    gemm_tiles<AG_RT, false, 8>(A.b, A.nks, ring, side, labels, q0, t0, (int)(t1 - t0), wave, lane,
+    gemm_tiles<false, 8>(A.b, A.nks, ring, side, labels, q0, t0, (int)(t1 - t0), wave, lane,
                              label, end);
 
     // ---- the two halves of the rows joined: maximum, then 16 columns (and the
@@ -554,7 +554,7 @@ bool plan_attend(int B, int N, int d, int dtype, int M, int n_cu, AttendPlan *p)
     const int ks = at_ks(dtype);
     p->dtype = dtype;
     p->nks = (d + ks - 1) / ks;
-    p->gemm = at_gemm(dtype, B, N, d, AG_REQS, n_cu);
+    p->gemm = at_gemm(dtype, B, N, d, n_cu);
     if (p->gemm) {
         p->nks = (d + AG_K - 1) / AG_K;
         p->ct = 1;

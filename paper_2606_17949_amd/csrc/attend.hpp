@@ -40,15 +40,15 @@ struct AttendPlan {
 };
 
 // Whether a batch goes by as a matrix product of tiles (attend_gemm.hpp) of 256
-// rows and `reqs` requests: more than half a tile of bf16 requests, of which
-// tiles for half the compute units, so that the scan by tiles of 64 would read
-// the bank three times or more. Forward, scan / tiles: 256 x 100,000 x 768 97 /
+// rows and 256 requests: more than half a tile of bf16 requests, for which the
+// scan by tiles of 64 would read the bank three times or more, and tiles for half
+// the compute units. Forward, scan / tiles: 256 x 100,000 x 768 97 /
 // 67 us, 512 x 100,000 x 384 95 / 83, but 128 x 100,000 x 768 59 / 67 and 150 x
 // 15,000 x 768 30 / 40.
-inline bool at_gemm(int dtype, int B, int N, int d, int reqs, int n_cu)
+inline bool at_gemm(int dtype, int B, int N, int d, int n_cu)
 {
-    const long tiles = ((long)N + 255) / 256 * ((B + reqs - 1) / reqs);
-    return dtype == 1 && d >= 128 && B > reqs / 2 && 2 * tiles >= n_cu;
+    const long tiles = ((long)N + 255) / 256 * ((B + 255) / 256);
+    return dtype == 1 && d >= 128 && B > 128 && 2 * tiles >= n_cu;
 }
 
 // Groups of 16 requests of a scan's tile: four where LDS holds them, fewer for a
@@ -100,9 +100,7 @@ hipError_t launch_zero(void *p, size_t bytes, hipStream_t s);   // bytes a multi
 // gradient ds (and what needs no further product), then d_queries += ds * rows,
 // then d_bank = ds^T * queries.
 struct GradPlan {
-    bool gemm;            // the first pass as a matrix product of tiles
     int dtype, ng, n_qt, n_chunks, waves, nks, slabs;
-    int n_gt;             // its request tiles (n_qt: tiles of ng groups, 64 of them a wave's)
     bool tab;             // the label gradients of a request tile fit LDS
     int n_blk;            // blocks of requests of one fragment of ds (32, fp32 16)
     int n_dt;             // fragments of 16 columns of a block of requests

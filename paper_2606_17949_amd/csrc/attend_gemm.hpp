@@ -8,13 +8,10 @@ namespace rb {
 
 namespace {
 
-constexpr int AG_ROWS = 256;   // bank rows of a workgroup's tile
-constexpr int AG_NG = 4;       // request groups of a wave
-constexpr int AG_K = 64;       // elements of a stage
-// requests of a tile whose waves have RT 16-row tiles each, bytes of a stage in LDS
-constexpr int ag_reqs(int rt) { return 8 / (AG_ROWS / (16 * rt)) * AG_NG * 16; }
-constexpr int ag_slot(int rt) { return (AG_ROWS + ag_reqs(rt)) * AG_K * 2; }
-constexpr int AG_RT = 8, AG_REQS = ag_reqs(AG_RT), AG_SLOT = ag_slot(AG_RT);
+constexpr int AG_ROWS = 256, AG_REQS = 256;   // of a workgroup's tile
+constexpr int AG_RT = 8, AG_NG = 4;           // 16-row tiles and request groups of a wave
+constexpr int AG_K = 64;                      // elements of a stage
+constexpr int AG_SLOT = (AG_ROWS + AG_REQS) * AG_K * 2;   // bytes of a stage in LDS
 
 // A lane number that the compiler takes for new: what is computed from it is
 // computed again each time, where kept through the products it would take the
@@ -42,14 +39,13 @@ __device__ __forceinline__ void dma4(const void *src, void *dst)
 }
 
 // A workgroup of 8 waves (two per SIMD) takes tiles of 256 bank rows against
-// its requests, a wave 16 * RT rows and 64 requests: with RT = 8, 256 requests
-// and 32 accumulators of 16 x 16 a wave, with 4, 128 and 16 (for kernels whose
-// work on a tile needs the registers). A stage brings 128 bytes of each of the
-// rows and requests into one of two LDS slots, whole lines (8 rows a load;
+// its 256 requests, wave w the 128 rows 128 * (w/4) .. and the 64 requests 64 *
+// (w%4) ..: 32 accumulators of 16 x 16. A stage brings 128 bytes of each of the
+// 512 rows and requests into one of two LDS slots, whole lines (8 rows a load;
 // row ri of load f keeps its 16-byte chunk c at 8*ri + (c ^ x), x one of 0, 1, 4,
 // 5 by row pair, ^ 2 in odd loads, so that a fragment read meets every bank
-// once). A stage is two k-steps of 32; of each a wave reads RT + 4 fragments for
-// 4 * RT MFMAs, every one while the products before it run, the first of a stage in the
+// once). A stage is two k-steps of 32; of each a wave reads 12 fragments for 32
+// MFMAs, every one while the products before it run, the first of a stage in the
 // stage before. The one barrier of a stage sits where its last fragments are
 // read: behind it the slot just read takes the stage after next and the next
 // stage's fragments come in.
@@ -62,19 +58,17 @@ __device__ __forceinline__ void dma4(const void *src, void *dst)
 // every wave: label(row, piece, lane) is a lane's address in piece `piece`, and they
 // land at labels + 64 * piece; end(tile, acc), behind the last stage, reads
 // them. nst: stages of a tile, at least 2.
-template <int RT, bool BANK_COLS, int LAB, typename Label, typename End>
+template <bool BANK_COLS, int LAB, typename Label, typename End>
 __device__ __forceinline__ void gemm_tiles(const AttendBank &A, int nst, uint8_t *ring,
                                            TileSide *side, float *labels, int q0, long tile0,
                                            int n_tiles, int wave, int lane, Label &&label,
                                            End &&end)
 {
     const uint32_t rowb = (uint32_t)A.d * 2;
-    constexpr int REQS = ag_reqs(RT), SLOT = ag_slot(RT), WQ = REQS / (AG_NG * 16);
-    constexpr int LOADS = (AG_ROWS + REQS) / 64, STEPS = 2 * RT;
-    static_assert(STEPS % 4 == 0, "four fragments of rows in turn");
-    const int wr = wave / WQ, wq = wave % WQ;
+    constexpr int RT = AG_RT, LOADS = 8, STEPS = 2 * RT;
+    const int wr = wave >> 2, wq = wave & 3;
     const int col = lane & 15, jg = lane >> 4;
-    const int nq = min(A.B - q0, REQS);
+    const int nq = min(A.B - q0, AG_REQS);
     const __amdgpu_buffer_rsrc_t rqr =
         make_rsrc(A.queries + (size_t)q0 * rowb, (uint32_t)nq * rowb);
     auto turn = [](int ri) { return ((ri >> 1) & 1) | ((ri >> 2) << 2); };   // 0, 1, 4, 5
@@ -152,13 +146,13 @@ __device__ __forceinline__ void gemm_tiles(const AttendBank &A, int nst, uint8_t
                 acc[i][g] = f32x4{0.f, 0.f, 0.f, 0.f};
     };
     issue(0);
-    issue(SLOT);
+    issue(AG_SLOT);
     wait_vmcnt<LOADS>();
     stream_barrier();
     uint32_t slot = 0;
     open(slot);
     for (int z = 0, tile = 0, kc = 0; z < n_stg; ++z) {
-        const uint32_t next = SLOT - slot;
+        const uint32_t next = AG_SLOT - slot;
         // the products of step n (row tile n % RT of k-step n / RT), and the reads
         // of the step after the next, behind the last of the next stage's
         auto products = [&](auto I) {

@@ -279,7 +279,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_gemm_kernel(const Us
             buffer_store4(to, jg == 0 ? (uint32_t)at * 4u : OFF_NONE, s);
         }
     };
-    gemm_tiles<AG_RT, true, 0>(A.b, A.nks, smem, side, nullptr, q0, t0, (int)(t1 - t0), wave, lane,
+    gemm_tiles<true, 0>(A.b, A.nks, smem, side, nullptr, q0, t0, (int)(t1 - t0), wave, lane,
                         [&](long, int, int) { return A.b.norms; }, end);
 }
 
@@ -611,80 +611,6 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_kernel(const DsArgs A)
     }
 }
 
-// The same as a matrix product of tiles, for large bf16 batches and at most 16
-// label columns; a tile's labels stand in LDS, [16 row tiles][4][64].
-constexpr int DS_RT = 4;
-
-__global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_gemm_kernel(const DsArgs A)
-{
-    constexpr int REQS = ag_reqs(DS_RT), WQ = REQS / 64;
-    extern __shared__ __align__(16) uint8_t smem[];
-    TileSide *side = (TileSide *)(smem + 2 * ag_slot(DS_RT));
-    float *sd = (float *)(side + 1);         // [3][REQS] hq, lse2, shift
-    float *tab = sd + 3 * REQS;              // [REQS / 16][4][64]
-    float *labels = tab + REQS / 16 * 4 * WAVE;
-    int t, ch;
-    chunk_and_tile(A.n_chunks, A.n_qt, &ch, &t);
-    if (ch >= A.n_chunks)
-        return;
-    const int tid = threadIdx.x, lane = tid & 63;
-    __builtin_assume(tid < AT_WAVES * WAVE);
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wr = wave / WQ, wq = wave % WQ;
-    const int q0 = t * REQS;
-    const int n_tiles = (int)((A.slabs + 7) / 8);   // of the part
-    const int t0 = (int)((long)ch * n_tiles / A.n_chunks),
-              t1 = (int)((long)(ch + 1) * n_tiles / A.n_chunks);
-    const int N = A.b.N, M = A.M;
-    load_side(A, q0, REQS, sd);
-    load_dout(A, q0, REQS, tab);
-    const long part0 = A.slab0 * AT_SLAB;   // first row of the part
-    float sum_ds[AG_NG][4], sum_db[AG_NG][4];
-#pragma unroll
-    for (int g = 0; g < AG_NG; ++g)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            sum_ds[g][e] = sum_db[g][e] = 0.f;
-    // the lane's address in piece 4*i + j of a tile's labels: row tile i, column
-    // 4*j + lane/16 (behind the last column, the first again)
-    auto label = [&](long row0, int f, int l) {
-        const long row = min(row0 + (f >> 2) * 16 + (l & 15), (long)N - 1);
-        const int cc = 4 * (f & 3) + (l >> 4);
-        return (cc < M || cc >= 2 * M ? A.qual : A.len) + row * M +
-               (cc < M ? cc : cc < 2 * M ? cc - M : 0);
-    };
-    auto end = [&](int tile, f32x4(&acc)[DS_RT][AG_NG]) {
-        const int l = fresh(lane);
-        const long row0 = part0 + (long)(t0 + tile) * AG_ROWS;
-        const int left = (int)min((long)AG_ROWS, N - row0);
-#pragma unroll
-        for (int r = 0; r < DS_RT; ++r) {
-            const int r16 = DS_RT * wr + r;   // row tile of the tile
-            const float nh = tile_norm(A.b, side, left, 16 * r16 + (l & 15));
-            const RowTile T{row0 + 16 * r16, (long)(t0 + tile) * 16 + r16,
-                            max(0, min(16, left - 16 * r16)), t * WQ + wq, q0 + 64 * wq};
-            auto lab = [&](int j) { return labels[(r16 * 4 + j) * WAVE + l]; };
-            ds_row_tile<AT_BF16, AG_NG>(A, T, sd + 64 * wq, REQS, tab + 4 * wq * A.n_j * WAVE, l,
-                                        nh, acc[r], lab, sum_ds, sum_db);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    gemm_tiles<DS_RT, true, 8>(A.b, A.nks, smem, side, labels, q0, A.slab0 / 8 + t0, t1 - t0, wave,
-                               lane, label, end);
-    // ---- the requests' sums, joined over the waves of a request
-    float *jn = (float *)smem;   // [8 / WQ][REQS][2]
-    stream_barrier();
-    put_sums<AG_NG>(sum_ds, sum_db, jn + (wr * REQS + 64 * wq) * 2, lane);
-    stream_barrier();
-    if (tid < 2 * REQS && q0 + tid / 2 < A.b.B) {   // request tid/2, sum tid%2
-        float s = 0.f;
-        for (int w = 0; w < AT_WAVES / WQ; ++w)
-            s += jn[w * 2 * REQS + tid];
-        float *to = A.req + ((size_t)ch * A.b.B + q0) * 2 + tid;
-        *to = A.first ? s : *to + s;
-    }
-}
-
 // Four elements of a gradient, rounded once.
 template <int DT>
 __device__ __forceinline__ void store4(uint8_t *base, size_t at, const f32x4 &v)
@@ -971,57 +897,96 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
     constexpr int LOADS = XL / 8 + SL / 8;
     for (int k = 0; k < SLOTS - 1; ++k)
         issue(z0 + k);
-    for (long z = z0; z < z1; ++z) {
-        __builtin_amdgcn_sched_barrier(0);
-        // slab z has landed for every wave, and slab z - 1 is read
+    if constexpr (DT == AT_BF16) {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef int i32x2 __attribute__((ext_vector_type(2)));
+        typedef __attribute__((address_space(3))) s16x4 *lds4;
+        auto across = [&](uint32_t at) {
+            return __builtin_bit_cast(
+                i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(smem + at)));
+        };
+        // 16 columns of the rows: four of 32 of them to a lane row, twice
+        const int ti = lane & 15, xrow = 4 * jg + (ti >> 2);
+        const uint32_t xat = (uint32_t)(xrow * ROWB + (ti & 1) * 8), xsw = (uint32_t)(xrow & 7) * 2;
+        auto read_x = [&](uint32_t slot, int i) {
+            i32x4 x;
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {   // (16 rows on, the same turn)
+                const uint32_t c16 = (uint32_t)(wd * 8 + i * 2) + ((ti >> 1) & 1);
+                const i32x2 w = across(slot + xat + r * 16 * ROWB + (c16 ^ xsw) * 16);
+                x[2 * r] = w[0];
+                x[2 * r + 1] = w[1];
+            }
+            return x;
+        };
+        // step n: value n % 2 (hi, lo) of group wq*4 + n/2, which is half n/2 % 2 of
+        // block wq*2 + n/4; the lane that wrote the four values this one reads
+        const uint32_t src = (uint32_t)ds_place((ti & 3) * 16 + 4 * jg + (ti >> 2)) * 16;
+        auto read_s = [&](uint32_t slot, int n) {
+            i32x4 s;
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const i32x2 w =
+                    across(slot + XB + ((r * NB + wq * 2 + n / 4) * 2 + n % 2) * 1024 + src +
+                           (uint32_t)(((n / 2) ^ jg) & 1) * 8);
+                s[2 * r] = w[0];
+                s[2 * r + 1] = w[1];
+            }
+            return s;
+        };
+        // A slab's eight steps of four MFMAs, each step's fragment read two steps
+        // ahead and the rows' in the second half of the slab before, so that the
+        // barrier, half way, finds fragments in registers.
+        i32x4 x[4], s[4];
         wait_vmcnt<(SLOTS - 2) * LOADS>();
         stream_barrier();
-        issue(z + SLOTS - 1);
         __builtin_amdgcn_sched_barrier(0);
-        const uint8_t *xb = smem + ((z - z0) % SLOTS) * (XB + SB), *sb = xb + XB;
-        if constexpr (DT == AT_BF16) {
-            typedef short s16x4 __attribute__((ext_vector_type(4)));
-            typedef int i32x2 __attribute__((ext_vector_type(2)));
-            typedef __attribute__((address_space(3))) s16x4 *lds4;
-            auto across = [](const uint8_t *p) {
-                return __builtin_bit_cast(i32x2,
-                                          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)p));
+        uint32_t slot = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            x[i] = read_x(slot, i);
+        s[0] = read_s(slot, 0);
+        s[1] = read_s(slot, 1);
+        for (long z = z0; z < z1; ++z) {
+            const uint32_t next =
+                slot == (uint32_t)(SLOTS - 1) * (XB + SB) ? 0u : slot + (XB + SB);
+            i32x4 y[4];
+            auto step = [&](auto I) {
+                constexpr int n = decltype(I)::value;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    acc[i][n / 2] = mfma_step<1>(x[i], s[n % 4], acc[i][n / 2]);
+                s[(n + 2) % 4] = n < 6 ? read_s(slot, n + 2) : read_s(next, n - 6);
+                if constexpr (n >= 4)
+                    y[n - 4] = read_x(next, n - 4);
+                __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, n >= 4 ? 4 : 2, 0);
             };
-            i32x4 a[4];
-            const int ti = lane & 15;
+            __builtin_amdgcn_sched_barrier(0);
+            static_for<0, 4>(step);
+            __builtin_amdgcn_sched_barrier(0);
+            // the next slab has landed for every wave, and the one before is read
+            wait_vmcnt<(SLOTS - 3) * LOADS>();
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            issue(z + SLOTS - 1);
+            __builtin_amdgcn_sched_barrier(0);
+            static_for<4, 8>(step);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const int row = r * 16 + 4 * jg + (ti >> 2);
-                    const int el = wd * 64 + i * 16 + 4 * (ti & 3);
-                    const i32x2 w = across(xb + row * ROWB +
-                                           ((el >> 3) ^ ((row & 7) * 2)) * 16 + (el & 7) * 2);
-                    a[i][2 * r] = w[0];
-                    a[i][2 * r + 1] = w[1];
-                }
-            // the lane that wrote the four values this one reads across
-            const int src = ds_place((ti & 3) * 16 + 4 * jg + (ti >> 2)) * 16;
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                // group wq*4 + g: half g & 1 of block wq*2 + g/2
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    i32x4 s;
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const i32x2 w =
-                            across(sb + ((r * NB + wq * 2 + (g >> 1)) * 2 + h) * 1024 + src +
-                                   ((g ^ jg) & 1) * 8);
-                        s[2 * r] = w[0];
-                        s[2 * r + 1] = w[1];
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        acc[i][g] = mfma_step<1>(a[i], s, acc[i][g]);
-                }
-            }
-        } else {
+                x[i] = y[i];
+            slot = next;
+        }
+    } else {
+        for (long z = z0; z < z1; ++z) {
+            __builtin_amdgcn_sched_barrier(0);
+            // slab z has landed for every wave, and slab z - 1 is read
+            wait_vmcnt<(SLOTS - 2) * LOADS>();
+            stream_barrier();
+            issue(z + SLOTS - 1);
+            __builtin_amdgcn_sched_barrier(0);
+            const uint8_t *xb = smem + ((z - z0) % SLOTS) * (XB + SB), *sb = xb + XB;
 #pragma unroll
             for (int r = 0; r < AT_RT; ++r) {
 #pragma unroll
@@ -1181,16 +1146,6 @@ hipError_t ds_one(const GradPlan &p, const DsArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-hipError_t ds_gemm(const GradPlan &p, const DsArgs &a, hipStream_t s)
-{
-    const hipError_t e = allow_lds(ds_gemm_kernel, p.lds_bytes);
-    if (e != hipSuccess)
-        return e;
-    hipLaunchKernelGGL(ds_gemm_kernel, dim3(p.n_chunks * p.n_gt), dim3(AT_WAVES * WAVE),
-                       p.lds_bytes, s, a);
-    return hipGetLastError();
-}
-
 template <int DT>
 hipError_t ds_dt(const GradPlan &p, const DsArgs &a, hipStream_t s)
 {
@@ -1262,7 +1217,7 @@ hipError_t run_grad(const GradPlan &p, const AttendBank &b, const GradArgs &g, u
     a.n_j = p.n_j;
     a.nks = p.nks;
     a.n_chunks = p.n_chunks;
-    a.n_qt = p.gemm ? p.n_gt : p.n_qt;
+    a.n_qt = p.n_qt;
     a.n_blk = p.n_blk;
     a.ds = g.d_queries || g.d_bank ? (i32x4 *)(wb + p.off_ds) : nullptr;
     a.rowsum = (float *)(wb + p.off_rowsum);
@@ -1281,7 +1236,7 @@ hipError_t run_grad(const GradPlan &p, const AttendBank &b, const GradArgs &g, u
         a.slab0 = z0;
         a.slabs = slabs;
         a.first = z0 == 0;
-        if ((e = p.gemm ? ds_gemm(p, a, s) : ds_dt<DT>(p, a, s)) != hipSuccess)
+        if ((e = ds_dt<DT>(p, a, s)) != hipSuccess)
             return e;
         if (g.d_queries) {
             DqArgs q{a.ds, b.rows, b.mask, b.B, b.d, p.n_blk, p.q_chunks, row0, nrows, slabs, dq,
@@ -1333,7 +1288,7 @@ bool plan_usage(int B, int N, int d, int dtype, int n_cu, UsagePlan *p)
     const int ks = at_ks(dtype);
     p->dtype = dtype;
     p->nks = (d + ks - 1) / ks;
-    p->gemm = at_gemm(dtype, B, N, d, AG_REQS, n_cu);
+    p->gemm = at_gemm(dtype, B, N, d, n_cu);
     p->off_side = 0;
     p->off_part = up256((size_t)B * sizeof(Side));
     if (p->gemm) {
@@ -1422,12 +1377,10 @@ bool plan_grad(int B, int N, int d, int dtype, int M, int n_cu, GradPlan *p)
     p->n_j = (2 * M + 15) / 16 * 4;
     const size_t group = (size_t)p->nks * ks * (dtype == AT_F32 ? 4 : 2) * 16 + 16 * sizeof(Side);
     const size_t tab = (size_t)p->n_j * WAVE * 4;
-    p->gemm = at_gemm(dtype, B, N, d, ag_reqs(DS_RT), n_cu) && 2 * M <= 16;
-    // (a wave of the tiled pass has 64 requests; a bf16 fragment of ds is of two
-    // groups, which one tile has to hold where there are two)
+    // (a bf16 fragment of ds is of two groups, which one tile has to hold where
+    // there are two)
     const int least = dtype == AT_BF16 && B > 16 ? 2 : 1;
-    const int ng =
-        p->gemm ? 4 : at_groups(B, N, group, n_cu, least, [](int) { return AT_SLAB; });
+    const int ng = at_groups(B, N, group, n_cu, least, [](int) { return AT_SLAB; });
     if (ng < least)
         return false;
     p->tab = (group + tab) * ng <= (size_t)AT_LDS;
@@ -1444,18 +1397,8 @@ bool plan_grad(int B, int N, int d, int dtype, int M, int n_cu, GradPlan *p)
         part = p->slabs;
     const int n_parts = (int)((p->slabs + part - 1) / part);
     part = (p->slabs + n_parts - 1) / n_parts;
-    if (p->gemm)   // (whole tiles)
-        part = (part + 7) / 8 * 8;
     p->part_slabs = (int)part;
-    p->n_gt = (B + ag_reqs(DS_RT) - 1) / ag_reqs(DS_RT);
-    if (p->gemm) {
-        p->nks = (d + AG_K - 1) / AG_K;
-        const long most = n_cu / p->n_gt, tiles256 = part / 8;
-        p->n_chunks = (int)(most < 1 ? 1 : most < tiles256 ? most : tiles256);
-        p->waves = AT_WAVES;
-    } else {
-        shares((int)part, AT_SLAB, dtype, d, p->n_qt, n_cu, &p->n_chunks, &p->waves);
-    }
+    shares((int)part, AT_SLAB, dtype, d, p->n_qt, n_cu, &p->n_chunks, &p->waves);
     const long tiles = (long)((d + DQ_COLS - 1) / DQ_COLS) *
                        ((B + DQ_GROUPS * 16 - 1) / (DQ_GROUPS * 16));
     long qc = n_cu / tiles;
@@ -1466,9 +1409,7 @@ bool plan_grad(int B, int N, int d, int dtype, int M, int n_cu, GradPlan *p)
     p->q_chunks = (int)(qc > part ? part : qc);
     const size_t lds = (group + (p->tab ? tab : 0)) * ng;
     const size_t join = (size_t)p->waves * ng * 16 * 2 * 4;
-    p->lds_bytes = p->gemm ? 2 * ag_slot(DS_RT) + sizeof(TileSide) + 3 * ag_reqs(DS_RT) * 4 +
-                                 (ag_reqs(DS_RT) / 16 + 16) * 4 * WAVE * 4
-                   : lds > join ? lds : join;
+    p->lds_bytes = lds > join ? lds : join;
     const int n_dt = (d + 31) / 32 * 2;
     p->n_dt = n_dt;
     if ((size_t)p->n_blk * n_dt * WAVE * 16 >= (size_t)1 << 31)   // (32-bit offsets)
