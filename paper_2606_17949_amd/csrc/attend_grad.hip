@@ -803,31 +803,36 @@ struct DqArgs {
     bool first;                // the first part sets part, the others add
 };
 
-constexpr int DQ_COLS = 256, DQ_GROUPS = 8;   // columns and request groups of a workgroup
-constexpr int DQ_MASKS = 1024;                // most slabs of a share
+constexpr int DQ_COLS = 256;     // columns of a workgroup
+constexpr int DQ_MASKS = 1024;   // most slabs of a share
 
-template <int DT> struct DqLayout {
+// NI: 16-column tiles of a wave, 4 or 8; its four groups of requests with it are
+// 4 * NI accumulators, and a workgroup's eight waves 2 * NI groups.
+template <int DT, int NI> struct DqLayout {
     static constexpr int H = DT == AT_BF16 ? 2 : 1;
     static constexpr int ESZ = DT == AT_F32 ? 4 : 2;
-    static constexpr int NB = DT == AT_BF16 ? DQ_GROUPS / 2 : DQ_GROUPS;   // blocks of requests
+    static constexpr int WD = 16 / NI, WQ = 8 / WD;          // waves over columns, requests
+    static constexpr int REQS = WQ * 64;
+    static constexpr int NB = REQS / (DT == AT_BF16 ? 32 : 16);   // blocks of requests
     static constexpr int ROWB = DQ_COLS * ESZ;               // bytes of a row in LDS
     static constexpr int XB = AT_SLAB * ROWB;                // of a slab's rows
     static constexpr int SB = AT_RT * NB * H * WAVE * 16;    // of its ds, [2][NB][H][64]
-    static constexpr int SLOTS = DT == AT_F32 ? 3 : 4;
+    static constexpr int SLOTS = XB + SB <= 32 * 1024 ? 4 : 3;
     static constexpr size_t BYTES = (size_t)SLOTS * (XB + SB) + DQ_MASKS * 4;
 };
 
 // Partial d_queries of a share of a part: sum over its rows of ds * row. A
-// workgroup of 8 waves has 256 columns x 128 requests, a wave 64 x 64; slabs of
-// 32 rows go through LDS, SLOTS - 1 ahead (with one ahead a slab's 512 cycles of
-// MFMA waited for memory: 256 x 100,000 x 768 took 164 us for less than half), and are read
+// workgroup of 8 waves has 256 columns x 128 or 256 requests, a wave 64 or 128
+// columns x 64; slabs of 32 rows go through LDS, two or three ahead, and are read
 // across (ds_read_b64_tr_b16: four rows of 16 columns become a column's four
 // rows per lane) for the product over rows: D[column 4*(lane/16) + e][request
-// lane % 16]. Masked rows hold anything and are not fetched: zeros.
-template <int DT>
+// lane % 16]. These reads bound it: a slab takes NI + 8 of 1 KB a wave for 8 * NI
+// MFMAs. (256 x 100,000 x 768 with NI = 4 107 us, with 8 87, and 7 more for the join of twice the shares.) Masked rows hold
+// anything and are not fetched: zeros.
+template <int DT, int NI>
 __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
 {
-    using L = DqLayout<DT>;
+    using L = DqLayout<DT, NI>;
     constexpr int H = L::H, ESZ = L::ESZ, ROWB = L::ROWB, XB = L::XB, SB = L::SB, NB = L::NB;
     constexpr int SLOTS = L::SLOTS;
     extern __shared__ __align__(16) uint8_t smem[];
@@ -835,7 +840,7 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, jg = lane >> 4;
-    const int wd = wave & 3, wq = wave >> 2;   // 64 columns, 4 groups of this wave
+    const int wd = wave % L::WD, wq = wave / L::WD;   // columns, requests of this wave
     // (a share's tiles run on one XCD: its rows and its ds come from memory once)
     const int n_ct = (A.d + DQ_COLS - 1) / DQ_COLS, n_bt = (A.n_blk + NB - 1) / NB;
     int ch, t;
@@ -855,9 +860,9 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
         }
         __syncthreads();
     }
-    f32x4 acc[4][4];
+    f32x4 acc[NI][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
             acc[i][g] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -912,7 +917,7 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
             i32x4 x;
 #pragma unroll
             for (int r = 0; r < 2; ++r) {   // (16 rows on, the same turn)
-                const uint32_t c16 = (uint32_t)(wd * 8 + i * 2) + ((ti >> 1) & 1);
+                const uint32_t c16 = (uint32_t)(wd * NI * 2 + i * 2) + ((ti >> 1) & 1);
                 const i32x2 w = across(slot + xat + r * 16 * ROWB + (c16 ^ xsw) * 16);
                 x[2 * r] = w[0];
                 x[2 * r + 1] = w[1];
@@ -934,33 +939,39 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
             }
             return s;
         };
-        // A slab's eight steps of four MFMAs, each step's fragment read two steps
-        // ahead and the rows' in the second half of the slab before, so that the
-        // barrier, half way, finds fragments in registers.
-        i32x4 x[4], s[4];
+        // A slab's eight steps of NI MFMAs, each step's fragment read two steps
+        // ahead, the rows' as the last step lets go of those before: the barrier,
+        // half way, finds fragments in registers.
+        i32x4 x[NI], s[4];
         wait_vmcnt<(SLOTS - 2) * LOADS>();
         stream_barrier();
         __builtin_amdgcn_sched_barrier(0);
         uint32_t slot = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < NI; ++i)
             x[i] = read_x(slot, i);
         s[0] = read_s(slot, 0);
         s[1] = read_s(slot, 1);
         for (long z = z0; z < z1; ++z) {
             const uint32_t next =
                 slot == (uint32_t)(SLOTS - 1) * (XB + SB) ? 0u : slot + (XB + SB);
-            i32x4 y[4];
             auto step = [&](auto I) {
                 constexpr int n = decltype(I)::value;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < NI; ++i) {
                     acc[i][n / 2] = mfma_step<1>(x[i], s[n % 4], acc[i][n / 2]);
+                    if constexpr (n == 7)
+                        x[i] = read_x(next, i);
+                }
                 s[(n + 2) % 4] = n < 6 ? read_s(slot, n + 2) : read_s(next, n - 6);
-                if constexpr (n >= 4)
-                    y[n - 4] = read_x(next, n - 4);
-                __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, n >= 4 ? 4 : 2, 0);
+                if constexpr (n == 7)
+                    static_for<0, NI>([&](auto) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                    });
+                else
+                    __builtin_amdgcn_sched_group_barrier(0x008, NI, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
             };
             __builtin_amdgcn_sched_barrier(0);
             static_for<0, 4>(step);
@@ -973,9 +984,6 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
             __builtin_amdgcn_sched_barrier(0);
             static_for<4, 8>(step);
             __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                x[i] = y[i];
             slot = next;
         }
     } else {
@@ -992,10 +1000,10 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int row = r * 16 + 4 * jg + e;
-                    float x[4], s[4];
+                    float x[NI], s[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int el = wd * 64 + i * 16 + col;
+                    for (int i = 0; i < NI; ++i) {
+                        const int el = wd * NI * 16 + i * 16 + col;
                         x[i] = *(const float *)(xb + row * ROWB + ((el >> 2) ^ (jg * 4)) * 16 +
                                                 (el & 3) * 4);
                     }
@@ -1006,7 +1014,7 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
                                                 ds_place(src) * 16 + (col & 3) * 4);
                     }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < NI; ++i)
 #pragma unroll
                         for (int g = 0; g < 4; ++g)
                             acc[i][g] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], s[g], acc[i][g],
@@ -1017,10 +1025,10 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
     }
     wait_vmcnt<0>();
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const int cc = c0 + wd * 64 + i * 16 + 4 * jg;
+            const int cc = c0 + (wd * NI + i) * 16 + 4 * jg;
             const int b = (DT == AT_BF16 ? b0 * 32 : b0 * 16) + (wq * 4 + g) * 16 + col;
             if (cc < A.d && b < A.B) {
                 f32x4 *at = (f32x4 *)(A.part + ((size_t)ch * A.B + b) * A.d + cc);
@@ -1192,6 +1200,20 @@ hipError_t dx_one(const DxArgs &x, hipStream_t s)
     return hipGetLastError();
 }
 
+template <int DT, int NI>
+hipError_t dq_one(const DqArgs &q, hipStream_t s)
+{
+    using L = DqLayout<DT, NI>;
+    const hipError_t e = allow_lds(dq_kernel<DT, NI>, L::BYTES);
+    if (e != hipSuccess)
+        return e;
+    hipLaunchKernelGGL((dq_kernel<DT, NI>),
+                       dim3(q.n_chunks * ((q.d + DQ_COLS - 1) / DQ_COLS) *
+                            ((q.n_blk + L::NB - 1) / L::NB)),
+                       dim3(512), L::BYTES, s, q);
+    return hipGetLastError();
+}
+
 template <int DT>
 hipError_t run_grad(const GradPlan &p, const AttendBank &b, const GradArgs &g, uint8_t *wb,
                     hipStream_t s)
@@ -1241,14 +1263,11 @@ hipError_t run_grad(const GradPlan &p, const AttendBank &b, const GradArgs &g, u
         if (g.d_queries) {
             DqArgs q{a.ds, b.rows, b.mask, b.B, b.d, p.n_blk, p.q_chunks, row0, nrows, slabs, dq,
                      z0 == 0};
-            using L = DqLayout<DT>;
-            if ((e = allow_lds(dq_kernel<DT>, L::BYTES)) != hipSuccess)
-                return e;
-            hipLaunchKernelGGL(dq_kernel<DT>,
-                               dim3(p.q_chunks * ((b.d + DQ_COLS - 1) / DQ_COLS) *
-                                    ((p.n_blk + L::NB - 1) / L::NB)),
-                               dim3(512), L::BYTES, s, q);
-            if ((e = hipGetLastError()) != hipSuccess)
+            if constexpr (DT == AT_BF16)
+                e = p.dq_wide ? dq_one<DT, 8>(q, s) : dq_one<DT, 4>(q, s);
+            else
+                e = dq_one<DT, 4>(q, s);
+            if (e != hipSuccess)
                 return e;
         }
         if (g.d_bank) {
@@ -1399,8 +1418,9 @@ bool plan_grad(int B, int N, int d, int dtype, int M, int n_cu, GradPlan *p)
     part = (p->slabs + n_parts - 1) / n_parts;
     p->part_slabs = (int)part;
     shares((int)part, AT_SLAB, dtype, d, p->n_qt, n_cu, &p->n_chunks, &p->waves);
-    const long tiles = (long)((d + DQ_COLS - 1) / DQ_COLS) *
-                       ((B + DQ_GROUPS * 16 - 1) / (DQ_GROUPS * 16));
+    p->dq_wide = dtype == AT_BF16 && B > 128;
+    const int dq_reqs = p->dq_wide ? 256 : 128;
+    const long tiles = (long)((d + DQ_COLS - 1) / DQ_COLS) * ((B + dq_reqs - 1) / dq_reqs);
     long qc = n_cu / tiles;
     qc = qc < 1 ? 1 : qc;
     // (a share's masks are kept in LDS)
