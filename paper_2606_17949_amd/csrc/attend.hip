@@ -7,11 +7,6 @@ namespace rb {
 
 namespace {
 
-// k-steps of bank rows in flight (4-bit rows: 128 elements each)
-constexpr int at_ring(int dt, int rt) { return dt == AT_Q4 || rt == 4 ? 2 : 4; }
-// 16-row tiles of a slab: 64 requests read each fragment of theirs from LDS for
-// 64 rows; with 32, LDS reads alone take as long as the products.
-constexpr int at_rt(int dt, int ng) { return dt != AT_F32 && ng == 4 ? 4 : 2; }
 // A running maximum is raised when a score passes it by this many powers of
 // two: weights stay below 2^16 and few slabs rescale what went before.
 constexpr float AT_SLACK = 16.f;
@@ -544,8 +539,6 @@ hipError_t launch_dt(const AttendPlan &p, const AttendArgs &a, hipStream_t s)
 {
     return p.ct == 1 ? launch_ng<DT, 1>(p, a, s) : launch_ng<DT, 2>(p, a, s);
 }
-
-size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 }  // namespace
 

@@ -8,14 +8,7 @@ namespace rb {
 
 namespace {
 
-// k-steps of bank rows in flight (4-bit rows: 128 elements each)
-constexpr int at_ring(int dt, int rt) { return dt == AT_Q4 || rt == 4 ? 2 : 4; }
-// 16-row tiles of a slab: 64 requests read each fragment of theirs from LDS for
-// 64 rows; with 32, LDS reads alone take as long as the products.
-constexpr int at_rt(int dt, int ng) { return dt != AT_F32 && ng == 4 ? 4 : 2; }
 constexpr size_t PART_BYTES = 128u << 20;   // ds of a part of the bank
-
-size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Per request: -|q|^2/2, lse in powers of two, and what is subtracted from the
 // weights' gradient, sum of the outputs' gradients times the outputs less the

@@ -32,6 +32,15 @@ inline __host__ __device__ uint32_t at_query_bytes(int dtype, int d)
     return (uint32_t)(dtype == AT_F32 ? d * 4 : d * 2);
 }
 
+// 16-row tiles of a slab: 64 requests read each fragment of theirs from LDS for
+// 64 rows; with 32, LDS reads alone take as long as the products.
+constexpr int at_rt(int dt, int ng) { return dt != AT_F32 && ng == 4 ? 4 : 2; }
+// k-steps of bank rows in flight (4-bit rows: 128 elements each; 64 requests over
+// 1,000,000 x 768 of them 148 us with one, 156 with two and spilled registers)
+constexpr int at_ring(int dt, int rt) { return dt == AT_Q4 ? (rt == 4 ? 1 : 3) : rt == 4 ? 2 : 4; }
+
+inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+
 // The request tile (NG groups of 16 from request q0 on, every k-step) into LDS:
 // qs[(k-step * SUB + sub) * NG + group][lane], lane (request lane % 16, K part
 // lane / 16). Zero past the batch and past the row.
