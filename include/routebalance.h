@@ -397,11 +397,13 @@ rb_status rb_route_batch_noalloc(const void *queries, const void *bank, const fl
  * Results are deterministic (sums in a fixed order, no floating atomics). B = 0
  * enqueues nothing but (rb_attend_usage) the decay and (rb_attend_backward) the
  * zeros of the gradients of the bank.
- * Errors shared by the calls: RB_ERR_DTYPE; RB_ERR_DIMS (B < 0, N < 1, d < 1,
+ * Scores 2*beta*<q, x> and beta*|x|^2 must stay within fp32 (below 3e38).
+ * Errors shared by the calls: RB_ERR_DTYPE; RB_ERR_DIMS (B < 0, B >= 2^24, N < 1, d < 1,
  * d > RB_MAX_D, d not a multiple of 4 for RB_F32, 8 for RB_BF16, 32 for RB_Q4,
  * M < 1, M > RB_MAX_M); RB_ERR_VALUE; RB_ERR_NULL; RB_ERR_ALIGN; RB_ERR_WORKSPACE;
  * RB_ERR_HIP. The *_workspace_size calls write the bytes for these sizes on the
- * current device to *bytes (a host pointer). */
+ * current device to *bytes (a host pointer): at least what any batch of up to B
+ * requests takes. */
 
 /* Predictions: q_hat[b][m] = sum_n p[b][n] * bank_qual[n][m], l_hat likewise from
  * bank_len, and lse[b] = log(sum_n exp(-beta*|q_b - x_n|^2)).
@@ -430,8 +432,9 @@ rb_status rb_attend(const void *queries, const void *bank, const uint8_t *scales
  * gradients of 0. Outputs are overwritten, and must not overlap the inputs. The
  * norms are taken as functions of the rows. dtype is RB_F32 or RB_BF16. For
  * bf16, ds enters the two products over d as a sum of two bf16 values (17 bits).
- * d_queries, d_bank 16-byte aligned. Batches whose requests, B and d rounded up
- * to multiples of 32, reach 2 GB are refused with RB_ERR_DIMS. */
+ * d_queries, d_bank 16-byte aligned. Batches whose requests reach 2 GB, B and d
+ * rounded up to multiples of 32 and d to at least 64, are refused with
+ * RB_ERR_DIMS. */
 rb_status rb_attend_backward_workspace_size(int B, int N, int d, rb_dtype dtype, int M,
                                             size_t *bytes);
 rb_status rb_attend_backward(const void *queries, const void *bank, const float *bank_norms,
@@ -477,8 +480,9 @@ rb_status rb_bank_evict(const float *usage, const uint8_t *may_go, int N, int n,
 
 /* New rows in place of old ones: row at[j] of the bank becomes new_rows[j], with
  * its norm, labels and, where usage is not NULL, usage0 as its usage; entries of
- * at outside [0, N) are passed over. The entries inside are distinct
- * (a precondition). Rows not named stay as they are.
+ * at outside [0, N) are passed over. The entries inside are distinct, and the new
+ * rows and labels lie outside the bank (preconditions). Rows not named stay as
+ * they are.
  *   at [n] int32; new_rows [n][d] of src_dtype, 16-byte aligned, which is dtype,
  *   or for a bank of RB_Q4 RB_F32 or RB_BF16 (held in 4 bits as by rb_bank_pack);
  *   new_qual, new_len [n][M] fp32; bank, scales, bank_norms, bank_qual, bank_len,

@@ -572,8 +572,14 @@ def _one_device(dev: torch.device, **tensors):
             raise ValueError(f"{name}: on {t.device}, the queries or the bank on {dev}")
 
 
-def _on(dev: torch.device):
-    """Makes ``dev`` current for the call (a no-op where it is)."""
+def _on(dev: torch.device, stream=None):
+    """Makes ``dev``, or ``stream`` on it, current for the call (a no-op where it
+    is): what the call allocates, workspaces that it lets go of at its end among
+    it, is then memory of the stream that uses it."""
+    if stream is not None:
+        if stream.device != dev:
+            raise ValueError(f"stream: on {stream.device}, the tensors on {dev}")
+        return torch.cuda.stream(stream)
     if dev.type != "cuda" or dev.index in (None, torch.cuda.current_device()):
         return contextlib.nullcontext()
     return torch.cuda.device(dev)
@@ -677,7 +683,7 @@ def rb_attend(queries, bank, bank_norms, beta: float, bank_qual, bank_len,
     dev = queries.device
     _one_device(dev, bank=bank, bank_norms=bank_norms, bank_qual=bank_qual, bank_len=bank_len,
                 scales=scales, row_mask=row_mask, q_hat=q_hat, l_hat=l_hat, lse=lse, ws=ws)
-    with _on(dev):
+    with _on(dev, stream):
         if q_hat is None:
             q_hat = torch.empty(B, M, dtype=torch.float32, device=dev)
         if l_hat is None:
@@ -723,7 +729,7 @@ def rb_attend_backward(queries, bank, bank_norms, beta: float, bank_qual, bank_l
     _one_device(dev, bank=bank, bank_norms=bank_norms, bank_qual=bank_qual, bank_len=bank_len,
                 row_mask=row_mask, q_hat=q_hat, l_hat=l_hat, lse=lse, dq_hat=dq_hat,
                 dl_hat=dl_hat, dlse=dlse, ws=ws, **{n: v[0] for n, v in out.items()})
-    with _on(dev):
+    with _on(dev, stream):
         made = all(v[0] is None for v in out.values())
         res = {n: torch.empty(shape, dtype=dt, device=dev) if made else t
                for n, (t, dt, shape) in out.items()}
@@ -752,7 +758,7 @@ def rb_attend_usage(queries, bank, bank_norms, beta: float, lse, usage, decay: f
     dev = queries.device
     _one_device(dev, bank=bank, bank_norms=bank_norms, scales=scales, row_mask=row_mask, lse=lse,
                 usage=usage, ws=ws)
-    with _on(dev):
+    with _on(dev, stream):
         if ws is None:
             ws = attend_usage_workspace(B, N, d, code, dev)
         _check(_lib.rb_attend_usage(_ptr(queries), _ptr(bank), _ptr(scales), _ptr(bank_norms), code,
@@ -776,7 +782,7 @@ def rb_bank_pack(bank, rows: Optional[torch.Tensor] = None, scales: Optional[tor
     _expect_opt(scales, torch.uint8, (N, d // 32), "scales")
     _expect_opt(norms, torch.float32, (N,), "norms")
     _one_device(dev, rows=rows, scales=scales, norms=norms)
-    with _on(dev):
+    with _on(dev, stream):
         if rows is None:
             rows = torch.empty(N, d // 2, dtype=torch.uint8, device=dev)
         if scales is None:
@@ -803,7 +809,7 @@ def rb_bank_evict(usage, n: int, may_go: Optional[torch.Tensor] = None,
         _expect(ws, torch.uint8, (ws.numel(),), "ws")
     dev = usage.device
     _one_device(dev, may_go=may_go, victims=victims, ws=ws)
-    with _on(dev):
+    with _on(dev, stream):
         if victims is None:
             victims = torch.empty(max(n, 0), dtype=torch.int32, device=dev)
         if ws is None:
@@ -835,7 +841,7 @@ def rb_bank_replace(at, new_rows, new_qual, new_len, bank, bank_norms, bank_qual
     _one_device(dev, at=at, new_rows=new_rows, new_qual=new_qual, new_len=new_len,
                 bank_norms=bank_norms, bank_qual=bank_qual, bank_len=bank_len, scales=scales,
                 usage=usage)
-    with _on(dev):
+    with _on(dev, stream):
         _check(_lib.rb_bank_replace(_ptr(at), n, _ptr(new_rows), src, _ptr(new_qual),
                                     _ptr(new_len), M, _ptr(bank), _ptr(scales), _ptr(bank_norms),
                                     code, N, d, _ptr(bank_qual), _ptr(bank_len), _ptr(usage),

@@ -279,13 +279,15 @@ rb_status route_batch(const void *queries, const void *bank, const float *bank_n
     return hip_status(e);
 }
 
+constexpr int MAX_B = (1 << 24) - 1;   // (a grid holds 2^32 threads: 256 join a request's parts)
+
 // Sizes of a bank that may also be held in 4 bits.
 rb_status check_attend_dims(rb_dtype dt, int B, int N, int d)
 {
     const rb_status s = check_embed_dims(dt == RB_Q4 ? RB_BF16 : dt, N, d);
     if (s != RB_OK)
         return s;
-    return B < 0 || (dt == RB_Q4 && d % 32 != 0) ? RB_ERR_DIMS : RB_OK;
+    return B < 0 || B > MAX_B || (dt == RB_Q4 && d % 32 != 0) ? RB_ERR_DIMS : RB_OK;
 }
 
 bool beta_ok(float beta) { return beta >= 1e-30f && beta <= 1e30f; }   // (no NaN)
@@ -321,6 +323,29 @@ rb_status attend_plan(P *p, F make)
     if (num_cu(&cu) != 0)
         return RB_ERR_HIP;
     return make(cu, p) ? RB_OK : RB_ERR_DIMS;
+}
+
+// The most workspace that a batch of up to B requests takes: a smaller batch can
+// take more than a larger one, as its few request tiles share the bank among more
+// workgroups. A plan's size grows with the batch between two multiples of 16 (the
+// smallest tile), and everywhere once the largest tiles (256 requests) fill the
+// device by themselves.
+template <typename P, typename F>
+rb_status attend_bytes(int B, size_t *bytes, F make)
+{
+    P p = {};
+    const rb_status s = attend_plan(&p, [&](int cu, P *q) {
+        size_t most = 0;
+        for (int b = 16; b < B && b <= 256 * cu; b += 16)
+            if (make(cu, b, q) && q->bytes > most)
+                most = q->bytes;
+        const bool ok = make(cu, B, q);
+        *bytes = most > q->bytes ? most : q->bytes;
+        return ok;
+    });
+    if (s != RB_OK)
+        *bytes = 0;
+    return s;
 }
 
 }  // namespace
@@ -609,13 +634,9 @@ rb_status rb_attend_workspace_size(int B, int N, int d, rb_dtype dtype, int M, s
     *bytes = 0;
     if (B == 0)
         return RB_OK;
-    rb::AttendPlan p;
-    s = attend_plan(&p, [&](int cu, rb::AttendPlan *q) {
-        return rb::plan_attend(B, N, d, (int)dtype, M, cu, q);
+    return attend_bytes<rb::AttendPlan>(B, bytes, [&](int cu, int b, rb::AttendPlan *q) {
+        return rb::plan_attend(b, N, d, (int)dtype, M, cu, q);
     });
-    if (s == RB_OK)
-        *bytes = p.bytes;
-    return s;
 }
 
 rb_status rb_attend(const void *queries, const void *bank, const uint8_t *scales,
@@ -657,18 +678,14 @@ rb_status rb_attend_backward_workspace_size(int B, int N, int d, rb_dtype dtype,
     rb_status s = check_embed_dims(dtype, N, d);
     if (s != RB_OK)
         return s;
-    if (B < 0 || M < 1 || M > RB_MAX_M)
+    if (B < 0 || B > MAX_B || M < 1 || M > RB_MAX_M)
         return RB_ERR_DIMS;
     *bytes = 0;
     if (B == 0)
         return RB_OK;
-    rb::GradPlan p;
-    s = attend_plan(&p, [&](int cu, rb::GradPlan *q) {
-        return rb::plan_grad(B, N, d, (int)dtype, M, cu, q);
+    return attend_bytes<rb::GradPlan>(B, bytes, [&](int cu, int b, rb::GradPlan *q) {
+        return rb::plan_grad(b, N, d, (int)dtype, M, cu, q);
     });
-    if (s == RB_OK)
-        *bytes = p.bytes;
-    return s;
 }
 
 rb_status rb_attend_backward(const void *queries, const void *bank, const float *bank_norms,
@@ -683,7 +700,7 @@ rb_status rb_attend_backward(const void *queries, const void *bank, const float 
     rb_status s = check_embed_dims(dtype, N, d);
     if (s != RB_OK)
         return s;
-    if (B < 0 || M < 1 || M > RB_MAX_M)
+    if (B < 0 || B > MAX_B || M < 1 || M > RB_MAX_M)
         return RB_ERR_DIMS;
     if (!beta_ok(beta))
         return RB_ERR_VALUE;
@@ -744,13 +761,9 @@ rb_status rb_attend_usage_workspace_size(int B, int N, int d, rb_dtype dtype, si
     *bytes = 0;
     if (B == 0)
         return RB_OK;
-    rb::UsagePlan p;
-    s = attend_plan(&p, [&](int cu, rb::UsagePlan *q) {
-        return rb::plan_usage(B, N, d, (int)dtype, cu, q);
+    return attend_bytes<rb::UsagePlan>(B, bytes, [&](int cu, int b, rb::UsagePlan *q) {
+        return rb::plan_usage(b, N, d, (int)dtype, cu, q);
     });
-    if (s == RB_OK)
-        *bytes = p.bytes;
-    return s;
 }
 
 rb_status rb_attend_usage(const void *queries, const void *bank, const uint8_t *scales,
@@ -836,12 +849,12 @@ rb_status rb_bank_replace(const int32_t *at, int n, const void *new_rows, rb_dty
                           float *bank_qual, float *bank_len, float *usage, float usage0,
                           void *stream)
 {
-    rb_status s = check_attend_dims(dtype, n, N, d);
+    rb_status s = check_attend_dims(dtype, 0, N, d);
     if (s != RB_OK)
         return s;
     if ((src_dtype != RB_F32 && src_dtype != RB_BF16) || (dtype != RB_Q4 && src_dtype != dtype))
         return RB_ERR_DTYPE;
-    if (M < 1 || M > RB_MAX_M)
+    if (n < 0 || M < 1 || M > RB_MAX_M)
         return RB_ERR_DIMS;
     if (!isfinite(usage0))
         return RB_ERR_VALUE;

@@ -578,8 +578,7 @@ bool plan_attend(int B, int N, int d, int dtype, int M, int n_cu, AttendPlan *p)
     // a wave's part of the bank stays under 1 GB (32-bit offsets)
     const long tiles = (long)p->n_qt * p->n_lt;
     long chunks = n_cu / tiles;
-    const long by_size =
-        ((long)p->slabs * slab * at_row_bytes(dtype, d) >> 30) / AT_WAVES + 1;
+    const long by_size = at_least_shares((long)p->slabs * slab, dtype, d);
     if (chunks < by_size)
         chunks = by_size;
     if (chunks > p->slabs)

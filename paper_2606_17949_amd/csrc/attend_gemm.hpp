@@ -256,12 +256,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t wave_rsrc(const void *base, ui
                      (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes));
 }
 
-// 4 bytes from or to a lane's place in a resource (0 from, nothing to past it).
-__device__ __forceinline__ float buffer_load4(__amdgpu_buffer_rsrc_t r, uint32_t at)
-{
-    return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (int)at, 0, 0));
-}
-
+// 4 bytes to a lane's place in a resource (nothing past it).
 __device__ __forceinline__ void buffer_store4(__amdgpu_buffer_rsrc_t r, uint32_t at, float v)
 {
     __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), r, (int)at, 0, 0);

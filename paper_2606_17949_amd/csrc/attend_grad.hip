@@ -21,6 +21,7 @@ struct Side {
 struct PrepArgs {
     const uint8_t *queries;
     int B, d, M, n_j;
+    int places;      // requests of whole tiles: what follows the batch is zeros
     const float *lse, *q_hat, *l_hat, *dq, *dl, *dlse;
     float *dout;     // label gradients as fragments (dout_place); null: not wanted
     Side *side;
@@ -39,8 +40,8 @@ __device__ __forceinline__ size_t dout_place(int b, int c, int n_j)
 template <int QDT>
 __device__ __forceinline__ void make_side(const PrepArgs &A, int b, int lane)
 {
-    if (b >= A.B) {   // (places of the last group)
-        if (A.dout && b < (A.B + 15) / 16 * 16)
+    if (b >= A.B) {
+        if (A.dout && b < A.places)
             for (int c = lane; c < 4 * A.n_j; c += WAVE)
                 A.dout[dout_place(b, c, A.n_j)] = 0.f;
         return;
@@ -306,7 +307,7 @@ struct DsArgs {
     const float *qual, *len;
     int M;
     const Side *side;
-    const float *dout;      // fragments, n_j pieces a group
+    const float *dout;      // fragments of whole tiles, n_j pieces a group
     int n_j;
     int nks, n_chunks, n_qt, n_blk;
     long slab0, slabs;      // this part
@@ -507,12 +508,12 @@ __device__ __forceinline__ void load_side(const DsArgs &A, int q0, int n, float 
     }
 }
 
-// The label gradients of n requests (whole groups) from q0 on into LDS.
+// The label gradients of a tile of n requests from q0 on into LDS.
 __device__ __forceinline__ void load_dout(const DsArgs &A, int q0, int n, float *tab)
 {
-    const int groups = (A.b.B + 15) / 16 - q0 / 16, per = A.n_j * WAVE;
+    const int per = A.n_j * WAVE;
     for (int i = threadIdx.x; i < n / 16 * per; i += blockDim.x)
-        tab[i] = i < groups * per ? A.dout[(size_t)(q0 / 16) * per + i] : 0.f;
+        tab[i] = A.dout[(size_t)(q0 / 16) * per + i];
 }
 
 // The pass by tiles of NG * 16 requests, as the forward one. TAB: their label
@@ -640,20 +641,20 @@ struct DxArgs {
     float scale;                   // 2 * beta
 };
 
-constexpr int DX_SLOTS = 4, DX_MOST = 16;   // slots of request fragments, most of them in one
+constexpr int DX_SLOTS = 4, DX_TILES = 8;   // slots of request fragments, of them in one
 
 // d_bank of a part: 2 beta (ds^T . q - x * sum of ds). A workgroup of 8 waves
-// has 256 rows x NC * 16 columns, a wave 32 rows of all the columns (up to 128
-// accumulator registers); the requests' fragments of a block (NC KB) go through
-// LDS, three blocks ahead, and a wave's fragments of ds straight into registers,
-// two ahead. A stage is 4 * NC MFMAs a wave, its LDS reads half of what the LDS
-// gives in that time.
-template <int DT, int NC>
+// has 256 rows x 128 columns, a wave 32 rows of all the columns; the requests'
+// fragments of a block (8 KB) go through LDS, three blocks ahead, and a wave's
+// fragments of ds straight into registers, two ahead. A stage is 32 MFMAs a wave
+// (bf16), its LDS reads half of what the LDS gives in that time.
+template <int DT>
 __global__ __launch_bounds__(512, 1) void dx_kernel(const DxArgs A)
 {
     constexpr int H = DT == AT_BF16 ? 2 : 1;   // values of ds
     constexpr int MDT = DT == AT_F32 ? 0 : 1;
-    constexpr int SLOT = (NC + 7) / 8 * 8 * WAVE;       // 16-byte places
+    constexpr int NC = DX_TILES;               // one fragment of a block to fetch a wave
+    constexpr int SLOT = NC * WAVE;            // 16-byte places
     __shared__ __align__(16) i32x4 ring[DX_SLOTS * SLOT];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -672,15 +673,11 @@ __global__ __launch_bounds__(512, 1) void dx_kernel(const DxArgs A)
         make_rsrc(A.ds + (any ? (r0 / 16) * A.n_blk * H * WAVE : 0),
                   any ? (uint32_t)(AT_RT * A.n_blk * H * WAVE * 16) : 0u);
     const uint32_t place = (uint32_t)ds_place(lane) * 16;
-    auto fetch = [&](int blk) {   // two fragments of block blk by this wave
-#pragma unroll
-        for (int j = 0; j < (NC + 7) / 8; ++j) {
-            const int f = wave + 8 * j;
-            dma16(rq, ring + (blk % DX_SLOTS) * SLOT + f * WAVE,
-                  blk < A.n_blk && f < NC && dt0 + f < A.n_dt
-                      ? (uint32_t)(((blk * A.n_dt + dt0 + f) * WAVE + lane) * 16)
-                      : OFF_NONE);
-        }
+    auto fetch = [&](int blk) {   // a fragment of block blk by this wave
+        dma16(rq, ring + (blk % DX_SLOTS) * SLOT + wave * WAVE,
+              blk < A.n_blk && dt0 + wave < A.n_dt
+                  ? (uint32_t)(((blk * A.n_dt + dt0 + wave) * WAVE + lane) * 16)
+                  : OFF_NONE);
     };
     i32x4 s[2][AT_RT][H];
     auto load_ds = [&](int blk, i32x4(&to)[AT_RT][H]) {
@@ -713,7 +710,7 @@ __global__ __launch_bounds__(512, 1) void dx_kernel(const DxArgs A)
             // this wave's part of the block and its ds are there once only what
             // was sent after them is outstanding; after the barrier every wave's
             // part is, and no wave reads the slot of the block before any more
-            wait_vmcnt<(NC + 7) / 8 + AT_RT * H>();
+            wait_vmcnt<1 + AT_RT * H>();
             stream_barrier();
             fetch(blk + 3);
             __builtin_amdgcn_sched_barrier(0);
@@ -820,8 +817,8 @@ template <int DT, int NI> struct DqLayout {
 // across (ds_read_b64_tr_b16: four rows of 16 columns become a column's four
 // rows per lane) for the product over rows: D[column 4*(lane/16) + e][request
 // lane % 16]. These reads bound it: a slab takes NI + 8 of 1 KB a wave for 8 * NI
-// MFMAs. (256 x 100,000 x 768 with NI = 4 107 us, with 8 87, and 7 more for the join of twice the shares.) Masked rows hold
-// anything and are not fetched: zeros.
+// MFMAs. (256 x 100,000 x 768 with NI = 4 107 us, with 8 87, and 7 more for the
+// join of twice the shares.) Masked rows hold anything and are not fetched: zeros.
 template <int DT, int NI>
 __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
 {
@@ -866,8 +863,8 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
         const long r0 = z * AT_SLAB;
         const bool in = z < z1;
         const int rows = in ? (int)min((long)AT_SLAB, A.nrows - r0) : 0;
-        const __amdgpu_buffer_rsrc_t rx = make_rsrc(A.rows + (size_t)(A.row0 + (in ? r0 : 0)) * rowb,
-                                                    (uint32_t)rows * rowb);
+        const __amdgpu_buffer_rsrc_t rx = make_rsrc(
+            A.rows + (size_t)(A.row0 + (in ? r0 : 0)) * rowb, (uint32_t)rows * rowb);
         const uint32_t live = A.mask && in ? keep[z - z0] : ~0u;
 #pragma unroll
         for (int j = 0; j < XL / 8; ++j) {
@@ -1163,7 +1160,7 @@ hipError_t ds_dt(const GradPlan &p, const DsArgs &a, hipStream_t s)
 void shares(int slabs, int slab, int dtype, int d, int n_qt, int n_cu, int *n_chunks, int *waves)
 {
     long chunks = n_cu / n_qt;
-    const long by_size = ((long)slabs * slab * at_row_bytes(dtype, d) >> 30) / AT_WAVES + 1;
+    const long by_size = at_least_shares((long)slabs * slab, dtype, d);
     if (chunks < by_size)
         chunks = by_size;
     if (chunks > slabs)
@@ -1178,18 +1175,19 @@ void shares(int slabs, int slab, int dtype, int d, int n_qt, int n_cu, int *n_ch
 template <int QDT>
 hipError_t run_prep(const PrepArgs &a, hipStream_t s)
 {
-    const int side_blocks = (a.B + 15) / 16 * 4;   // (whole groups)
+    const int side_blocks = (a.places + 3) / 4;
     const long frags = a.qpack ? (long)a.n_blk * a.n_dt * WAVE : 0;
     hipLaunchKernelGGL(prep_kernel<QDT>, dim3((unsigned)(side_blocks + (frags + 255) / 256)),
                        dim3(256), 0, s, a, side_blocks);
     return hipGetLastError();
 }
 
-template <int DT, int NC>
+template <int DT>
 hipError_t dx_one(const DxArgs &x, hipStream_t s)
 {
-    hipLaunchKernelGGL((dx_kernel<DT, NC>), dim3(x.n_row_blocks * ((x.n_dt + NC - 1) / NC)),
-                       dim3(512), 0, s, x);
+    hipLaunchKernelGGL(dx_kernel<DT>,
+                       dim3(x.n_row_blocks * ((x.n_dt + DX_TILES - 1) / DX_TILES)), dim3(512), 0,
+                       s, x);
     return hipGetLastError();
 }
 
@@ -1216,9 +1214,9 @@ hipError_t run_grad(const GradPlan &p, const AttendBank &b, const GradArgs &g, u
     float *dout = (float *)(wb + p.off_dout);
     i32x4 *qpack = (i32x4 *)(wb + p.off_qpack);
     const int n_dt = p.n_dt;
-    hipError_t e = run_prep<QDT>({b.queries, b.B, b.d, g.M, p.n_j, g.lse, g.q_hat, g.l_hat,
-                                  g.dq_hat, g.dl_hat, g.dlse, dout, side, p.n_blk, n_dt,
-                                  g.d_bank ? qpack : nullptr},
+    hipError_t e = run_prep<QDT>({b.queries, b.B, b.d, g.M, p.n_j, p.n_qt * p.ng * 16, g.lse,
+                                  g.q_hat, g.l_hat, g.dq_hat, g.dl_hat, g.dlse, dout, side,
+                                  p.n_blk, n_dt, g.d_bank ? qpack : nullptr},
                                  s);
     if (e != hipSuccess)
         return e;
@@ -1267,19 +1265,15 @@ hipError_t run_grad(const GradPlan &p, const AttendBank &b, const GradArgs &g, u
             DxArgs x{a.ds, qpack, a.rowsum, b.rows, b.mask, (uint8_t *)g.d_bank, p.n_blk, n_dt,
                      p.n_qt, b.d, a.part_rows, row0, nrows,
                      (int)((nrows + 8 * AT_SLAB - 1) / (8 * AT_SLAB)), scale};
-            // as many columns to a workgroup as leave few of the last one's idle
-            const int per = (n_dt + (n_dt + DX_MOST - 1) / DX_MOST - 1) /
-                            ((n_dt + DX_MOST - 1) / DX_MOST);
-            e = dx_one<DT, 8>(x, s);
-            if (e != hipSuccess)
+            if ((e = dx_one<DT>(x, s)) != hipSuccess)
                 return e;
         }
     }
     if (g.d_queries || g.d_beta) {
         hipLaunchKernelGGL(dq_join_kernel<DT>,
-                           dim3(b.B, g.d_queries ? (b.d + 255) / 256 : 1), dim3(256), 0, s, dq, p.q_chunks, a.req,
-                           p.n_chunks, b.queries, b.B, b.d, scale, (uint8_t *)g.d_queries,
-                           g.d_beta);
+                           dim3(b.B, g.d_queries ? (b.d + 255) / 256 : 1), dim3(256), 0, s, dq,
+                           p.q_chunks, a.req, p.n_chunks, b.queries, b.B, b.d, scale,
+                           (uint8_t *)g.d_queries, g.d_beta);
         if ((e = hipGetLastError()) != hipSuccess)
             return e;
     }
@@ -1303,6 +1297,7 @@ bool plan_usage(int B, int N, int d, int dtype, int n_cu, UsagePlan *p)
     p->gemm = at_gemm(dtype, B, N, d, n_cu);
     p->off_side = 0;
     p->off_part = up256((size_t)B * sizeof(Side));
+    const size_t group = (size_t)p->nks * ks * (dtype == AT_F32 ? 4 : 2) * 16 + 16 * sizeof(Side);
     if (p->gemm) {
         p->nks = (d + AG_K - 1) / AG_K;
         p->n_qt = (B + AG_REQS - 1) / AG_REQS;
@@ -1314,7 +1309,6 @@ bool plan_usage(int B, int N, int d, int dtype, int n_cu, UsagePlan *p)
         p->bytes = p->off_part + up256((size_t)p->n_part * N * 4);
         return true;
     }
-    const size_t group = (size_t)p->nks * ks * (dtype == AT_F32 ? 4 : 2) * 16 + 16 * sizeof(Side);
     const int ng = at_groups(B, N, group, n_cu, 1, [&](int g) { return 16 * at_rt(dtype, g); });
     if (ng == 0)
         return false;
@@ -1335,7 +1329,7 @@ hipError_t launch_usage(const UsagePlan &p, const AttendBank &b, const float *ls
     Side *side = (Side *)((uint8_t *)ws + p.off_side);
     PrepArgs pa{};
     pa.queries = b.queries;
-    pa.B = b.B;
+    pa.B = pa.places = b.B;
     pa.d = b.d;
     pa.lse = lse;
     pa.side = side;
@@ -1358,8 +1352,8 @@ hipError_t launch_usage(const UsagePlan &p, const AttendBank &b, const float *ls
                              : usage_dt<AT_Q4>(p, a, s);
     if (e != hipSuccess || !a.part)
         return e;
-    hipLaunchKernelGGL(usage_join_kernel, dim3((unsigned)(((long)b.N + 255) / 256)), dim3(256), 0, s, a.part,
-                       p.n_part, b.N, decay, usage);
+    hipLaunchKernelGGL(usage_join_kernel, dim3((unsigned)(((long)b.N + 255) / 256)), dim3(256), 0,
+                       s, a.part, p.n_part, b.N, decay, usage);
     return hipGetLastError();
 }
 
@@ -1425,19 +1419,24 @@ bool plan_grad(int B, int N, int d, int dtype, int M, int n_cu, GradPlan *p)
     p->lds_bytes = lds > join ? lds : join;
     const int n_dt = (d + 31) / 32 * 2;
     p->n_dt = n_dt;
-    if ((size_t)p->n_blk * n_dt * WAVE * 16 >= (size_t)1 << 31)   // (32-bit offsets)
+    // (32-bit offsets into the requests' fragments and into a slab's ds)
+    if ((size_t)p->n_blk * (n_dt > 4 ? n_dt : 4) * WAVE * 16 >= (size_t)1 << 31)
         return false;
     size_t o = 0;
     p->off_side = o;
     o += up256((size_t)B * sizeof(Side));
     p->off_dout = o;
-    o += up256((size_t)((B + 15) / 16) * tab);
+    o += up256((size_t)p->n_qt * ng * tab);
     p->off_qpack = o;
     o += up256((size_t)p->n_blk * n_dt * WAVE * 16);
     p->off_ds = o;
-    o += up256((size_t)part * slab_ds);
+    // (a part as large as any, so that the size grows with B: a slab has at least
+    // 2048 bytes of ds for 16 requests, and 128 of sums for a request tile)
+    const size_t n16 = ((size_t)B + 15) / 16, all = (size_t)p->slabs;
+    const size_t room = PART_BYTES > slab_ds ? PART_BYTES : slab_ds;
+    o += up256(all * slab_ds < room ? all * slab_ds : room);
     p->off_rowsum = o;
-    o += up256((size_t)p->n_qt * part * AT_SLAB * 4);
+    o += up256(all * n16 * 128 < room / 16 ? all * n16 * 128 : room / 16);
     p->off_lab = o;
     o += p->n_qt > 1 ? up256((size_t)p->n_qt * N * M * 8) : 0;
     p->off_req = o;

@@ -39,6 +39,12 @@ constexpr int at_rt(int dt, int ng) { return dt != AT_F32 && ng == 4 ? 4 : 2; }
 // 1,000,000 x 768 of them 148 us with one, 156 with two and spilled registers)
 constexpr int at_ring(int dt, int rt) { return dt == AT_Q4 ? (rt == 4 ? 1 : 3) : rt == 4 ? 2 : 4; }
 
+// Shares of a bank whose waves' parts stay under 1 GB (32-bit offsets).
+inline long at_least_shares(long rows, int dtype, int d)
+{
+    return (rows * at_row_bytes(dtype, d) >> 30) / AT_WAVES + 1;
+}
+
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // The request tile (NG groups of 16 from request q0 on, every k-step) into LDS:
@@ -82,7 +88,8 @@ __device__ __forceinline__ i32x4 widen4(uint32_t codes, float scale)
 // request tile in LDS. Bank rows come from HBM straight into MFMA operand
 // registers, R k-steps (a block) ahead across slab ends, and no wave waits for
 // another once the request tile, sent for before the call, has landed; ready()
-// is called then, in every wave. side(slab) sends for what end(slab, acc) reads beside the products.
+// is called then, in every wave. side(slab) sends for what end(slab, acc) reads
+// beside the products.
 // A slab's first block stands apart from the others: there the compiler knows
 // that side's loads came after the block's own, so that waiting for the block
 // does not wait for them. (In one loop over all blocks every slab emptied the
@@ -91,7 +98,8 @@ __device__ __forceinline__ i32x4 widen4(uint32_t codes, float scale)
 // BANK_COLS false: acc[r][g][e] is <q, x> of row 16*r + 4*(lane/16) + e and
 // request 16*g + lane%16; true: of row 16*r + lane%16 and request
 // 16*g + 4*(lane/16) + e.
-template <int DT, int NG, int RT, int R, bool BANK_COLS, typename Ready, typename Side, typename End>
+template <int DT, int NG, int RT, int R, bool BANK_COLS, typename Ready, typename Side,
+          typename End>
 __device__ __forceinline__ void scan_slabs(const AttendBank &A, int nks, const i32x4 *qs, long s0,
                                            long s1, int lane, Ready &&ready, Side &&side,
                                            End &&end)
