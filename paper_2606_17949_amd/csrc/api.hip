@@ -311,7 +311,8 @@ rb::AttendBank attend_bank(const void *queries, const void *bank, const uint8_t 
     a.B = B;
     a.N = N;
     a.d = d;
-    a.c = (float)(2.0 * (double)beta * 1.4426950408889634);
+    a.beta = beta;
+    a.c = (float)a.c_exact();
     return a;
 }
 
@@ -745,7 +746,6 @@ rb_status rb_attend_backward(const void *queries, const void *bank, const float 
     g.d_qual = d_qual;
     g.d_len = d_len;
     g.d_beta = d_beta;
-    g.beta = beta;
     return hip_status(rb::launch_grad(
         p, attend_bank(queries, bank, nullptr, bank_norms, row_mask, B, N, d, beta), g, ws,
         (hipStream_t)stream));

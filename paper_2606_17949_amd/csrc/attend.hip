@@ -403,11 +403,12 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
 __global__ __launch_bounds__(256) void attend_join_kernel(const float *ml, const float *o,
                                                           int n_chunks, int n_lt, int width, int B,
                                                           int M, const uint8_t *queries, int qbytes,
-                                                          bool bf16, float c, float *q_hat,
-                                                          float *l_hat, float *lse)
+                                                          bool bf16, double c, double more,
+                                                          float *q_hat, float *l_hat, float *lse)
 {
-    __shared__ float red[256], wts[256], part[3][4];
+    __shared__ float red[256], wts[256], part[2][4];
     const int b = blockIdx.x, tid = threadIdx.x, wave = tid >> 6;
+    __shared__ double squares[4];
     const int col = tid & 15, row = tid >> 4;
     // the block's maximum or sum of one value a thread
     auto over = [&](int which, float v, auto op, float none) {
@@ -459,11 +460,17 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const float *ml, const
     }
     const float total = over(1, sum, [](float u, float v) { return u + v; }, 0.f);
     if (lse) {
-        // the maximum and c*|q|^2/2 nearly cancel: in 64 bits
-        q2 = over(2, q2, [](float u, float v) { return u + v; }, 0.f);
-        if (tid == 0)
-            lse[b] = (float)((double)m - 0.5 * (double)c * (double)q2 +
-                             (double)__builtin_amdgcn_logf(total)) * LN2;
+        // the maximum and c*|q|^2/2 nearly cancel: in 64 bits, with what rounding c
+        // took from them
+        const double w2 = wave_sum64(q2);
+        if ((tid & 63) == 0)
+            squares[wave] = w2;
+        __syncthreads();
+        if (tid == 0) {
+            const double s2 = (squares[0] + squares[1]) + (squares[2] + squares[3]);
+            lse[b] = (float)(((m - 0.5 * c * s2) * more + __builtin_amdgcn_logf(total)) *
+                             0.6931471805599453);
+        }
     }
     for (int c0 = 0; c0 < 2 * M; c0 += 16) {
         float s = 0.f;
@@ -619,7 +626,7 @@ hipError_t launch_attend(const AttendPlan &p, const AttendBank &b, const float *
         return e;
     hipLaunchKernelGGL(attend_join_kernel, dim3(b.B), dim3(256), 0, s, a.ml, a.o, p.n_chunks,
                        p.n_lt, 16 * p.ct, b.B, M, b.queries, (int)at_query_bytes(p.dtype, b.d),
-                       p.dtype != AT_F32, b.c, q_hat, l_hat, lse);
+                       p.dtype != AT_F32, (double)b.c, b.c_exact() / b.c, q_hat, l_hat, lse);
     return hipGetLastError();
 }
 

@@ -24,7 +24,8 @@ struct AttendBank {
     const float *norms;
     const uint8_t *mask;                      // [N] or null
     int B, N, d;
-    float c;                                  // 2 * beta * log2(e)
+    float beta, c;                            // c: 2 * beta * log2(e), rounded
+    double c_exact() const { return 2.0 * (double)beta * 1.4426950408889634; }
 };
 
 struct AttendPlan {
@@ -118,7 +119,6 @@ struct GradArgs {
     const float *q_hat, *l_hat, *lse, *dq_hat, *dl_hat, *dlse;   // dlse may be null
     void *d_queries, *d_bank;                                    // may be null
     float *d_qual, *d_len, *d_beta;                              // may be null
-    float beta;
 };
 
 bool plan_grad(int B, int N, int d, int dtype, int M, int n_cu, GradPlan *p);

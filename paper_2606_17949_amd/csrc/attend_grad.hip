@@ -27,6 +27,7 @@ struct PrepArgs {
     Side *side;
     int n_blk, n_dt; // fragments of the requests, [n_blk][n_dt][64]
     i32x4 *qpack;
+    double c, more;  // the passes' c, and what it lacks, over c
 };
 
 // The label gradients as MFMA fragments, [group of 16 requests][n_j][64]: column
@@ -51,28 +52,38 @@ __device__ __forceinline__ void make_side(const PrepArgs &A, int b, int lane)
     float s = 0.f;
     for (int i = lane; i < n16; i += WAVE)
         s = sumsq16<QDT>(load16(q + (size_t)i * 16), s);
-    s = wave_sum(s);
+    const double s2 = wave_sum64(s);
     const float lse = A.lse[b];
     const bool alive = lse != -INFINITY;
-    float dot = 0.f;
+    const float lse2 = alive ? lse * LOG2E : INFINITY;
+    // What rounding lse2 and c takes from the exponent of a row near the request
+    // (c * a about lse2), of a request's weights as a whole: up to 2^-23 of lse2.
+    // The gradients are linear in the weights, and get it with the outputs' ones;
+    // for the usage it goes into hq.
+    const double lost =
+        alive ? A.more * (double)lse2 - ((double)lse * 1.4426950408889634 - (double)lse2) : 0.0;
+    const float f = __builtin_amdgcn_exp2f((float)lost);
+    double dot = 0.0;
     if (A.dout) {
         // (a dead request's outputs are no numbers, and its gradients may be none)
         for (int c = lane; c < 4 * A.n_j; c += WAVE) {
             float g = 0.f, o = 0.f;
             if (alive && c < 2 * A.M) {
                 const size_t at = (size_t)b * A.M + (c < A.M ? c : c - A.M);
-                g = c < A.M ? A.dq[at] : A.dl[at];
+                g = f * (c < A.M ? A.dq[at] : A.dl[at]);
                 o = c < A.M ? A.q_hat[at] : A.l_hat[at];
             }
-            dot = fmaf(g, o, dot);
+            dot += (double)g * (double)o;
             A.dout[dout_place(b, c, A.n_j)] = g;
         }
-        dot = wave_sum(dot);
+        // (one rounding of it, which every row's gradient of this request shares)
+        dot = wave_sum64(dot);
         if (alive && A.dlse)
-            dot -= A.dlse[b];
+            dot -= (double)f * (double)A.dlse[b];
     }
     if (lane == 0)
-        A.side[b] = Side{-0.5f * s, alive ? lse * LOG2E : INFINITY, dot, 0.f};
+        A.side[b] =
+            Side{(float)((A.dout ? 0.0 : lost / A.c) - 0.5 * s2), lse2, (float)dot, 0.f};
 }
 
 // Fragments of the requests for d_bank: [block of requests][16 columns][64]
@@ -199,7 +210,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_kernel(const UsageAr
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     sum += __builtin_amdgcn_exp2f(
-                        fmaf(c, acc[r][g][e] + (nh + hq[g][e]), -lse2[g][e]));
+                        fmaf(c, (acc[r][g][e] + nh) + hq[g][e], -lse2[g][e]));
             sum = rows_reduce(sum, [](float x, float y) { return x + y; });
             if (masked && mk[r] == 0)
                 sum = 0.f;
@@ -261,7 +272,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_gemm_kernel(const Us
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     sum[r] += __builtin_amdgcn_exp2f(
-                        fmaf(c, acc[r][g][e] + (nh + hq[e]), -lse2[e]));
+                        fmaf(c, (acc[r][g][e] + nh) + hq[e], -lse2[e]));
             }
         }
 #pragma unroll
@@ -389,7 +400,7 @@ __device__ __forceinline__ void ds_row_tile(const DsArgs &A, const RowTile &T, c
         float ds[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float a = live ? sc[g][e] + (nh + hq[e]) : 0.f;
+            const float a = live ? (sc[g][e] + nh) + hq[e] : 0.f;
             const float p = live ? __builtin_amdgcn_exp2f(fmaf(c, a, -lse2[e])) : 0.f;
             ds[e] = p * dp[g][e];
             sc[g][e] = p;
@@ -1216,7 +1227,8 @@ hipError_t run_grad(const GradPlan &p, const AttendBank &b, const GradArgs &g, u
     const int n_dt = p.n_dt;
     hipError_t e = run_prep<QDT>({b.queries, b.B, b.d, g.M, p.n_j, p.n_qt * p.ng * 16, g.lse,
                                   g.q_hat, g.l_hat, g.dq_hat, g.dl_hat, g.dlse, dout, side,
-                                  p.n_blk, n_dt, g.d_bank ? qpack : nullptr},
+                                  p.n_blk, n_dt, g.d_bank ? qpack : nullptr, b.c,
+                                  b.c_exact() / b.c - 1.0},
                                  s);
     if (e != hipSuccess)
         return e;
@@ -1241,7 +1253,7 @@ hipError_t run_grad(const GradPlan &p, const AttendBank &b, const GradArgs &g, u
     a.d_len = g.d_len && p.n_qt > 1 ? lab + n_lab * p.n_qt : g.d_len;
     a.req = (float *)(wb + p.off_req);
     float *dq = (float *)(wb + p.off_dq);
-    const float scale = 2.f * g.beta;
+    const float scale = 2.f * b.beta;
     for (int z0 = 0; z0 < p.slabs; z0 += p.part_slabs) {
         const int slabs = p.slabs - z0 < p.part_slabs ? p.slabs - z0 : p.part_slabs;
         const long row0 = (long)z0 * AT_SLAB;
@@ -1333,6 +1345,8 @@ hipError_t launch_usage(const UsagePlan &p, const AttendBank &b, const float *ls
     pa.d = b.d;
     pa.lse = lse;
     pa.side = side;
+    pa.c = b.c;
+    pa.more = b.c_exact() / b.c - 1.0;
     hipError_t e = p.dtype == AT_F32 ? run_prep<0>(pa, s) : run_prep<1>(pa, s);
     if (e != hipSuccess)
         return e;

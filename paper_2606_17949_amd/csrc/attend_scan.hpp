@@ -10,7 +10,7 @@ namespace {
 
 constexpr int AT_RT = 2;                 // 16-row tiles of a fragment of ds
 constexpr int AT_SLAB = 16 * AT_RT;
-constexpr float LN2 = 0.693147180559945309f, LOG2E = 1.442695040888963407f;
+constexpr float LOG2E = 1.442695040888963407f;
 
 // What 16 bytes of a bank row per lane are (a k-step: 64 bytes of each of 16
 // rows), and how many request fragments of 16 bytes per lane meet them.
@@ -46,6 +46,26 @@ inline long at_least_shares(long rows, int dtype, int d)
 }
 
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Sum over the wave in 64 bits, in the order of wave_reduce.
+__device__ __forceinline__ double wave_sum64(double v)
+{
+    auto plus = [](double x, auto move) {
+        const uint64_t b = __builtin_bit_cast(uint64_t, x);
+        return x + __builtin_bit_cast(double, (uint64_t)move((uint32_t)(b >> 32)) << 32 |
+                                                  move((uint32_t)b));
+    };
+    v = plus(v, [](uint32_t w) { return dpp<0xb1>(w); });
+    v = plus(v, [](uint32_t w) { return dpp<0x4e>(w); });
+    v = plus(v, [](uint32_t w) { return dpp<0x141>(w); });
+    v = plus(v, [](uint32_t w) { return dpp<0x140>(w); });
+    v = plus(v, [](uint32_t w) { return dpp<0x142, 0xa>(w); });
+    v = plus(v, [](uint32_t w) { return dpp<0x143, 0xc>(w); });
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(
+        double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), 63) << 32 |
+                    (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, 63));
+}
 
 // The request tile (NG groups of 16 from request q0 on, every k-step) into LDS:
 // qs[(k-step * SUB + sub) * NG + group][lane], lane (request lane % 16, K part
@@ -161,9 +181,24 @@ __device__ __forceinline__ void scan_slabs(const AttendBank &A, int nks, const i
     __builtin_amdgcn_sched_barrier(0);
     ready();
 
-    f32x4 acc[RT][NG];
+    // A block's products are summed by themselves: a score is then a sum of few
+    // partial sums, and off by what those few additions round away. (One chain of
+    // 256 products of four fp32 elements: 12 requests over 1,473 x 1,024 at beta 21
+    // had gradients off by 2e-5 in their weights, now 3e-6. 64 requests' tiles have
+    // no registers for it.)
+    constexpr bool PARTS = RT == 2;
+    f32x4 acc[RT][NG], sum[PARTS ? RT : 1][PARTS ? NG : 1];
+    auto clear = [&](auto &x) {
+#pragma unroll
+        for (auto &row : x)
+#pragma unroll
+            for (auto &v : row)
+                v = f32x4{0.f, 0.f, 0.f, 0.f};
+    };
     // the products of block b, and the loads of the block after it
     auto block = [&](int b) {
+        if constexpr (PARTS)
+            clear(acc);
         static_for<0, R>([&](auto U) {
             constexpr int u = decltype(U)::value;
             __builtin_amdgcn_sched_barrier(0);
@@ -192,20 +227,26 @@ __device__ __forceinline__ void scan_slabs(const AttendBank &A, int nks, const i
             });
             issue(U);
         });
+        if constexpr (PARTS)
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+                    sum[r][g] = b == 0 ? acc[r][g] : sum[r][g] + acc[r][g];
         advance();
     };
     for (int slab = 0; slab < n_slabs; ++slab) {
         side(slab);
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int g = 0; g < NG; ++g)
-                acc[r][g] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (!PARTS)
+            clear(acc);
         block(0);
         __builtin_amdgcn_sched_barrier(0);
         for (int b = 1; b < n_blk; ++b)
             block(b);
-        end(slab, acc);
+        if constexpr (PARTS)
+            end(slab, sum);
+        else
+            end(slab, acc);
     }
 }
 
