@@ -108,7 +108,7 @@ struct GradPlan {
     int n_j;              // pieces of 4 label columns, a multiple of four
     int part_slabs;       // slabs of a part
     int q_chunks;         // shares of a part in the d_queries pass
-    bool dq_wide;         // its tiles hold 256 requests, not 128
+    int dq_reqs;          // requests of its tiles: 32, 64, 128 or 256
     size_t lds_bytes;
     size_t off_side, off_dout, off_qpack, off_ds, off_rowsum, off_lab, off_req, off_dq, bytes;
 };

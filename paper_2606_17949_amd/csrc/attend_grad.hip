@@ -658,12 +658,15 @@ constexpr int DX_SLOTS = 4, DX_TILES = 8;   // slots of request fragments, of th
 // has 256 rows x 128 columns, a wave 32 rows of all the columns; the requests'
 // fragments of a block (8 KB) go through LDS, three blocks ahead, and a wave's
 // fragments of ds straight into registers, two ahead. A stage is 32 MFMAs a wave
-// (bf16), its LDS reads half of what the LDS gives in that time.
+// (bf16), its LDS reads half of what the LDS gives in that time. Few requests are
+// bound by the bank's way in and d_bank's out (16 over 100,000 x 768 bf16 60 us, 5.1
+// TB/s); 256, at 115 us, have 31 us of MFMAs, 65 of memory and, six times, ds from
+// L2. (With each row's loads waited for by themselves at the end they took 134.)
 template <int DT>
 __global__ __launch_bounds__(512, 1) void dx_kernel(const DxArgs A)
 {
     constexpr int H = DT == AT_BF16 ? 2 : 1;   // values of ds
-    constexpr int MDT = DT == AT_F32 ? 0 : 1;
+    constexpr int MDT = DT == AT_F32 ? 0 : 1, ESZ = DT == AT_F32 ? 4 : 2;
     constexpr int NC = DX_TILES;               // one fragment of a block to fetch a wave
     constexpr int SLOT = NC * WAVE;            // 16-byte places
     __shared__ __align__(16) i32x4 ring[DX_SLOTS * SLOT];
@@ -749,50 +752,73 @@ __global__ __launch_bounds__(512, 1) void dx_kernel(const DxArgs A)
             load_ds(blk + 2, s[u]);
         });
     }
-    wait_vmcnt<0>();   // (no global-to-LDS load in flight when the workgroup ends)
+    // (all of a wave's rows are sent for before the first is used; rows and columns
+    // past the end load zeros and are not stored)
+    const uint32_t rowb = (uint32_t)A.d * ESZ;
+    const int left = any ? (int)min((long)AT_SLAB, A.nrows - r0) : 0;
+    const size_t first = (size_t)(A.row0 + (any ? r0 : 0)) * rowb;
+    const __amdgpu_buffer_rsrc_t rx = make_rsrc(A.rows + first, (uint32_t)left * rowb);
+    const __amdgpu_buffer_rsrc_t to = make_rsrc(A.d_bank + first, (uint32_t)left * rowb);
+    auto byte = [&](int r, int k, int h) {
+        const int c0 = dealt_column(dt0 + k, 4 * jg) + 4 * h;
+        return c0 < A.d ? (uint32_t)(r * 16 + col) * rowb + (uint32_t)c0 * ESZ : OFF_NONE;
+    };
+    constexpr int HX = DT == AT_F32 ? 2 : 1;   // 16-byte pieces of eight columns
+    i32x4 x[AT_RT][NC / 2][HX];
+#pragma unroll
+    for (int r = 0; r < AT_RT; ++r)
+#pragma unroll
+        for (int k = 0; k < NC; k += 2)
+#pragma unroll
+            for (int h = 0; h < HX; ++h)
+                x[r][k / 2][h] = buffer_load16(rx, byte(r, k, h));
+    float sum[AT_RT];
+    bool live[AT_RT];
 #pragma unroll
     for (int r = 0; r < AT_RT; ++r) {
-        const long lr = r0 + r * 16 + col;
-        if (lr >= A.nrows)
-            continue;
-        float sum = 0.f;
-        for (int t = 0; t < A.n_qt; ++t)
-            sum += A.rowsum[(size_t)t * A.part_rows + lr];
-        const size_t row = (size_t)(A.row0 + lr);
-        const bool live = !A.mask || A.mask[row] != 0;
-        // (eight columns a lane: 16 rows x 64 bytes an instruction of bf16; four at a
-        // time took 160 us for 131 at 256 x 100,000 x 768)
+        const long lr = min(r0 + r * 16 + col, A.nrows - 1);
+        live[r] = !A.mask || A.mask[A.row0 + lr] != 0;
+        sum[r] = 0.f;
+        // (a lane row every fourth tile, four in flight)
+#pragma unroll 4
+        for (int t = jg; t < A.n_qt; t += 4)
+            sum[r] += A.rowsum[(size_t)t * A.part_rows + lr];
+    }
+#pragma unroll
+    for (int r = 0; r < AT_RT; ++r)
+        sum[r] = rows_reduce(sum[r], [](float u, float v) { return u + v; });
+    wait_vmcnt<0>();   // (no global-to-LDS load in flight when the workgroup ends)
+    // eight columns a lane: 16 rows x 64 bytes an instruction of bf16 (four at a
+    // time took 160 us for 131 at 256 x 100,000 x 768)
+#pragma unroll
+    for (int r = 0; r < AT_RT; ++r)
 #pragma unroll
         for (int k = 0; k < NC; k += 2) {
-            const int c0 = dealt_column(dt0 + k, 4 * jg);
-            if (c0 >= A.d)
-                continue;
-            const size_t at = row * A.d + c0;
-            f32x4 v[2];
-            auto result = [&](int h, const f32x4 &x) {
+            float y[8];
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    v[h][e] = live ? A.scale * (acc[r][k + h][e] - x[e] * sum) : 0.f;
-            };
+            for (int e = 0; e < 8; ++e) {
+                const int w = x[r][k / 2][DT == AT_F32 ? e / 4 : 0][DT == AT_F32 ? e % 4 : e / 2];
+                const float v = DT == AT_F32 ? __int_as_float(w)
+                                : e % 2      ? bf16hi((uint32_t)w)
+                                             : bf16lo((uint32_t)w);
+                y[e] = live[r] ? A.scale * (acc[r][k + e / 4][e % 4] - v * sum[r]) : 0.f;
+            }
             if constexpr (DT == AT_BF16) {
-                const i32x4 x = load16(A.rows + at * 2);
-                result(0, f32x4{bf16lo(x[0]), bf16hi(x[0]), bf16lo(x[1]), bf16hi(x[1])});
-                result(1, f32x4{bf16lo(x[2]), bf16hi(x[2]), bf16lo(x[3]), bf16hi(x[3])});
-                bf16x8 y;
+                bf16x8 z;
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    y[e] = (__bf16)v[e >> 2][e & 3];
-                *(bf16x8 *)(A.d_bank + at * 2) = y;
+                    z[e] = (__bf16)y[e];
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, z), to,
+                                                       (int)byte(r, k, 0), 0, 0);
             } else {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
-                    if (c0 + 4 * h < A.d) {
-                        result(h, load4<DT>(A.rows, at + 4 * h));
-                        store4<DT>(A.d_bank, at + 4 * h, v[h]);
-                    }
+                    __builtin_amdgcn_raw_buffer_store_b128(
+                        __builtin_bit_cast(i32x4, f32x4{y[4 * h], y[4 * h + 1], y[4 * h + 2],
+                                                        y[4 * h + 3]}),
+                        to, (int)byte(r, k, h), 0, 0);
             }
         }
-    }
 }
 
 struct DqArgs {
@@ -807,13 +833,14 @@ struct DqArgs {
 constexpr int DQ_COLS = 256;     // columns of a workgroup
 constexpr int DQ_MASKS = 1024;   // most slabs of a share
 
-// NI: 16-column tiles of a wave, 4 or 8; its four groups of requests with it are
-// 4 * NI accumulators, and a workgroup's eight waves 2 * NI groups.
-template <int DT, int NI> struct DqLayout {
+// NI: 16-column tiles of a wave; G: groups of 16 requests of it. Its accumulators
+// are 4 * NI * G, and a workgroup's eight waves have 256 columns and NI * G / 2
+// groups.
+template <int DT, int NI, int G> struct DqLayout {
     static constexpr int H = DT == AT_BF16 ? 2 : 1;
     static constexpr int ESZ = DT == AT_F32 ? 4 : 2;
     static constexpr int WD = 16 / NI, WQ = 8 / WD;          // waves over columns, requests
-    static constexpr int REQS = WQ * 64;
+    static constexpr int REQS = WQ * G * 16;
     static constexpr int NB = REQS / (DT == AT_BF16 ? 32 : 16);   // blocks of requests
     static constexpr int ROWB = DQ_COLS * ESZ;               // bytes of a row in LDS
     static constexpr int XB = AT_SLAB * ROWB;                // of a slab's rows
@@ -823,17 +850,17 @@ template <int DT, int NI> struct DqLayout {
 };
 
 // Partial d_queries of a share of a part: sum over its rows of ds * row. A
-// workgroup of 8 waves has 256 columns x 128 or 256 requests, a wave 64 or 128
-// columns x 64; slabs of 32 rows go through LDS, two or three ahead, and are read
-// across (ds_read_b64_tr_b16: four rows of 16 columns become a column's four
+// workgroup of 8 waves has 256 columns x 32 to 256 requests, a wave 16 * NI
+// columns x 16 * G; slabs of 32 rows go through LDS, two or three ahead, and are
+// read across (ds_read_b64_tr_b16: four rows of 16 columns become a column's four
 // rows per lane) for the product over rows: D[column 4*(lane/16) + e][request
-// lane % 16]. These reads bound it: a slab takes NI + 8 of 1 KB a wave for 8 * NI
-// MFMAs. (256 x 100,000 x 768 with NI = 4 107 us, with 8 87, and 7 more for the
+// lane % 16]. With many requests these reads bound it: a slab takes NI + 2 * G of 1
+// KB a wave for 2 * G * NI MFMAs; with few, the rows' way from memory. (256 x 100,000 x 768 with NI = 4 107 us, with 8 87, and 7 more for the
 // join of twice the shares.) Masked rows hold anything and are not fetched: zeros.
-template <int DT, int NI>
+template <int DT, int NI, int G>
 __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
 {
-    using L = DqLayout<DT, NI>;
+    using L = DqLayout<DT, NI, G>;
     constexpr int H = L::H, ESZ = L::ESZ, ROWB = L::ROWB, XB = L::XB, SB = L::SB, NB = L::NB;
     constexpr int SLOTS = L::SLOTS;
     extern __shared__ __align__(16) uint8_t smem[];
@@ -861,14 +888,16 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
         }
         __syncthreads();
     }
-    f32x4 acc[NI][4];
+    f32x4 acc[NI][G];
 #pragma unroll
     for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
+        for (int g = 0; g < G; ++g)
             acc[i][g] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    constexpr int XL = XB / 1024, SL = SB / 1024;   // loads of 64 x 16 bytes
+    // loads of 64 x 16 bytes: the rows', ds's, and how many of these a wave sends for
+    // (all waves as many: of four pieces each goes out twice, to one place)
+    constexpr int XL = XB / 1024, SL = SB / 1024, SW = (SL + 7) / 8;
     auto issue = [&](long z) {
         uint8_t *buf = smem + ((z - z0) % SLOTS) * (XB + SB);
         const long r0 = z * AT_SLAB;
@@ -891,8 +920,8 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
             make_rsrc(A.ds + (size_t)(in ? z : 0) * AT_RT * A.n_blk * H * WAVE,
                       in ? (uint32_t)(AT_RT * A.n_blk * H * WAVE * 16) : 0u);
 #pragma unroll
-        for (int j = 0; j < SL / 8; ++j) {
-            const int f = wave * (SL / 8) + j;
+        for (int j = 0; j < SW; ++j) {
+            const int f = (wave * SW + j) % SL;
             const int r = f / (NB * H), rest = f % (NB * H);
             const int blk = b0 + rest / H, h = rest % H;
             dma16(rs, (i32x4 *)(buf + XB + f * 1024),
@@ -900,7 +929,7 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
                                 : OFF_NONE);
         }
     };
-    constexpr int LOADS = XL / 8 + SL / 8;
+    constexpr int LOADS = XL / 8 + SW;
     for (int k = 0; k < SLOTS - 1; ++k)
         issue(z0 + k);
     if constexpr (DT == AT_BF16) {
@@ -925,24 +954,25 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
             }
             return x;
         };
-        // step n: value n % 2 (hi, lo) of group wq*4 + n/2, which is half n/2 % 2 of
-        // block wq*2 + n/4; the lane that wrote the four values this one reads
+        // step n: value n % 2 (hi, lo) of group wq*G + n/2, which is half n/2 % 2 of
+        // block wq*G/2 + n/4; the lane that wrote the four values this one reads
         const uint32_t src = (uint32_t)ds_place((ti & 3) * 16 + 4 * jg + (ti >> 2)) * 16;
         auto read_s = [&](uint32_t slot, int n) {
             i32x4 s;
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 const i32x2 w =
-                    across(slot + XB + ((r * NB + wq * 2 + n / 4) * 2 + n % 2) * 1024 + src +
+                    across(slot + XB + ((r * NB + wq * (G / 2) + n / 4) * 2 + n % 2) * 1024 + src +
                            (uint32_t)(((n / 2) ^ jg) & 1) * 8);
                 s[2 * r] = w[0];
                 s[2 * r + 1] = w[1];
             }
             return s;
         };
-        // A slab's eight steps of NI MFMAs, each step's fragment read two steps
+        // A slab's 2 * G steps of NI MFMAs, each step's fragment read two steps
         // ahead, the rows' as the last step lets go of those before: the barrier,
         // half way, finds fragments in registers.
+        constexpr int NS = 2 * G;
         i32x4 x[NI], s[4];
         wait_vmcnt<(SLOTS - 2) * LOADS>();
         stream_barrier();
@@ -961,11 +991,12 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
 #pragma unroll
                 for (int i = 0; i < NI; ++i) {
                     acc[i][n / 2] = mfma_step<1>(x[i], s[n % 4], acc[i][n / 2]);
-                    if constexpr (n == 7)
+                    if constexpr (n == NS - 1)
                         x[i] = read_x(next, i);
                 }
-                s[(n + 2) % 4] = n < 6 ? read_s(slot, n + 2) : read_s(next, n - 6);
-                if constexpr (n == 7)
+                s[(n + 2) % 4] =
+                    n < NS - 2 ? read_s(slot, n + 2) : read_s(next, n + 2 - NS);
+                if constexpr (n == NS - 1)
                     static_for<0, NI>([&](auto) {
                         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
                         __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
@@ -975,7 +1006,7 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
                 __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
             };
             __builtin_amdgcn_sched_barrier(0);
-            static_for<0, 4>(step);
+            static_for<0, NS / 2>(step);
             __builtin_amdgcn_sched_barrier(0);
             // the next slab has landed for every wave, and the one before is read
             wait_vmcnt<(SLOTS - 3) * LOADS>();
@@ -983,7 +1014,7 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
             __builtin_amdgcn_sched_barrier(0);
             issue(z + SLOTS - 1);
             __builtin_amdgcn_sched_barrier(0);
-            static_for<4, 8>(step);
+            static_for<NS / 2, NS>(step);
             __builtin_amdgcn_sched_barrier(0);
             slot = next;
         }
@@ -1001,7 +1032,7 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int row = r * 16 + 4 * jg + e;
-                    float x[NI], s[4];
+                    float x[NI], s[G];
 #pragma unroll
                     for (int i = 0; i < NI; ++i) {
                         const int el = wd * NI * 16 + i * 16 + col;
@@ -1009,15 +1040,15 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
                                                 (el & 3) * 4);
                     }
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
+                    for (int g = 0; g < G; ++g) {
                         const int src = (col >> 2) * 16 + 4 * jg + e;
-                        s[g] = *(const float *)(sb + (r * NB + wq * 4 + g) * 1024 +
+                        s[g] = *(const float *)(sb + (r * NB + wq * G + g) * 1024 +
                                                 ds_place(src) * 16 + (col & 3) * 4);
                     }
 #pragma unroll
                     for (int i = 0; i < NI; ++i)
 #pragma unroll
-                        for (int g = 0; g < 4; ++g)
+                        for (int g = 0; g < G; ++g)
                             acc[i][g] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], s[g], acc[i][g],
                                                                              0, 0, 0);
                 }
@@ -1028,9 +1059,9 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
 #pragma unroll
     for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
+        for (int g = 0; g < G; ++g) {
             const int cc = c0 + (wd * NI + i) * 16 + 4 * jg;
-            const int b = (DT == AT_BF16 ? b0 * 32 : b0 * 16) + (wq * 4 + g) * 16 + col;
+            const int b = (DT == AT_BF16 ? b0 * 32 : b0 * 16) + (wq * G + g) * 16 + col;
             if (cc < A.d && b < A.B) {
                 f32x4 *at = (f32x4 *)(A.part + ((size_t)ch * A.B + b) * A.d + cc);
                 *at = A.first ? acc[i][g] : *at + acc[i][g];
@@ -1202,14 +1233,14 @@ hipError_t dx_one(const DxArgs &x, hipStream_t s)
     return hipGetLastError();
 }
 
-template <int DT, int NI>
+template <int DT, int NI, int G>
 hipError_t dq_one(const DqArgs &q, hipStream_t s)
 {
-    using L = DqLayout<DT, NI>;
-    const hipError_t e = allow_lds(dq_kernel<DT, NI>, L::BYTES);
+    using L = DqLayout<DT, NI, G>;
+    const hipError_t e = allow_lds(dq_kernel<DT, NI, G>, L::BYTES);
     if (e != hipSuccess)
         return e;
-    hipLaunchKernelGGL((dq_kernel<DT, NI>),
+    hipLaunchKernelGGL((dq_kernel<DT, NI, G>),
                        dim3(q.n_chunks * ((q.d + DQ_COLS - 1) / DQ_COLS) *
                             ((q.n_blk + L::NB - 1) / L::NB)),
                        dim3(512), L::BYTES, s, q);
@@ -1267,9 +1298,14 @@ hipError_t run_grad(const GradPlan &p, const AttendBank &b, const GradArgs &g, u
             DqArgs q{a.ds, b.rows, b.mask, b.B, b.d, p.n_blk, p.q_chunks, row0, nrows, slabs, dq,
                      z0 == 0};
             if constexpr (DT == AT_BF16)
-                e = p.dq_wide ? dq_one<DT, 8>(q, s) : dq_one<DT, 4>(q, s);
+                e = p.dq_reqs == 256   ? dq_one<DT, 8, 4>(q, s)
+                    : p.dq_reqs == 128 ? dq_one<DT, 4, 4>(q, s)
+                    : p.dq_reqs == 64  ? dq_one<DT, 2, 4>(q, s)
+                                       : dq_one<DT, 2, 2>(q, s);
             else
-                e = dq_one<DT, 4>(q, s);
+                e = p.dq_reqs == 128  ? dq_one<DT, 4, 4>(q, s)
+                    : p.dq_reqs == 64 ? dq_one<DT, 2, 4>(q, s)
+                                      : dq_one<DT, 2, 2>(q, s);
             if (e != hipSuccess)
                 return e;
         }
@@ -1419,8 +1455,11 @@ bool plan_grad(int B, int N, int d, int dtype, int M, int n_cu, GradPlan *p)
     part = (p->slabs + n_parts - 1) / n_parts;
     p->part_slabs = (int)part;
     shares((int)part, AT_SLAB, dtype, d, p->n_qt, n_cu, &p->n_chunks, &p->waves);
-    p->dq_wide = dtype == AT_BF16 && B > 128;
-    const int dq_reqs = p->dq_wide ? 256 : 128;
+    // (the requests of a tile that the batch does not have cost what the others do:
+    // tiles of 128 for 1 to 32 requests took 21 us for 10 over 14,919 x 384 fp32, 46
+    // for 33 over 100,000 x 768 bf16, and for 64 of these 51 for 43)
+    p->dq_reqs = B <= 32 ? 32 : B <= 64 ? 64 : B <= 128 || dtype == AT_F32 ? 128 : 256;
+    const int dq_reqs = p->dq_reqs;
     const long tiles = (long)((d + DQ_COLS - 1) / DQ_COLS) * ((B + dq_reqs - 1) / dq_reqs);
     long qc = n_cu / tiles;
     qc = qc < 1 ? 1 : qc;

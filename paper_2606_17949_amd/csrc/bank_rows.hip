@@ -105,17 +105,32 @@ __global__ __launch_bounds__(256) void write_rows_kernel(const RowsArgs A)
 
 // ---- the n least of N, by three histograms of the ordered bits of the keys
 // (11, 11 and 10 of them), which leave the n-th least key T and how many of
-// those equal to it are taken; then every block counts its rows below T and at
-// T, and writes its own behind those of the blocks before it. What bounds it is
-// latency: five passes over 4 bytes a row, each a launch. Usage falls into few
-// of the first histogram's bins (of one exponent and two bits of mantissa), so
+// those equal to it are taken; then every block writes its rows below T, and its
+// share of those at T, behind those of the blocks before it. What bounds it is
+// latency: four passes over 4 bytes a row, each a launch. Usage falls into few of
+// the first histogram's bins (of one exponent and two bits of mantissa), so
 // blocks add to one of EV_COPIES histograms, and the n-th key's bin is found by
 // every block of the next pass for itself (found by the last block of a pass to
 // arrive, with a counter and fences between, a pass over 4,000,000 rows took 42
-// us).
+// us). With few blocks each has a first histogram of its own, which nothing has to
+// clear before (64 of 40,000 rows 20.4 us for 22.9, of 130,000 23.1 for 23.4; 61
+// blocks with one each 28.4 for 22.6); the first pass clears the other two. The
+// third leaves, block by block, how many rows come before each of its bins: the
+// last pass needs no pass before it that counts them (with one, 10 of 10,000 took
+// 22.0 us for 19.1, 50,000 of 4,000,000 35.5 for 34.0).
 constexpr int EV_BINS = 2048, EV_THREADS = 1024, EV_COPIES = 8;
 constexpr int EV_TILE = EV_THREADS * 4;   // rows a block takes at a time, four a thread
 constexpr int EV_BLOCKS = 256;            // most blocks
+constexpr int EV_OWN = 32;                // most blocks with a first histogram each
+constexpr int EV_LAST = 1024, EV_CUM = EV_LAST + 1;   // bins of the last histogram
+
+// Workspace in 32-bit words: the states, the histograms of the second and third
+// pass, those of the first (one each or EV_COPIES), [blocks][EV_CUM] rows before
+// the third's bins.
+constexpr int EV_HIST = EV_COPIES * EV_BINS;
+constexpr int EV_AT_HIST = 64, EV_AT_FIRST = EV_AT_HIST + 2 * EV_HIST;
+constexpr int EV_AT_CUM = EV_AT_FIRST + EV_OWN * EV_BINS;
+static_assert(EV_OWN >= EV_COPIES, "room of the first histograms");
 
 // Where the search stands behind each histogram: the bits of T found so far,
 // the rows to take among those with these bits, and whether there are fewer
@@ -155,9 +170,9 @@ __device__ __forceinline__ Four load_four(const float *usage, const uint8_t *may
     return f;
 }
 
-__global__ __launch_bounds__(EV_THREADS) void evict_clear_kernel(uint32_t *hist)
+__global__ __launch_bounds__(EV_THREADS) void evict_clear_kernel(uint32_t *ws)
 {
-    hist[blockIdx.x * EV_THREADS + threadIdx.x] = 0;
+    ws[EV_AT_FIRST + blockIdx.x * EV_THREADS + threadIdx.x] = 0;
 }
 
 constexpr int ev_bits(int level) { return level == 2 ? 10 : 11; }
@@ -166,7 +181,7 @@ constexpr int ev_shift(int level) { return level == 0 ? 21 : level == 1 ? 10 : 0
 // The state behind histogram L, from the one before it (L 0: n rows to take).
 // Every thread of the block gets it.
 template <int L>
-__device__ __forceinline__ EvictState evict_pick(const uint32_t *hist_all, EvictState st)
+__device__ __forceinline__ EvictState evict_pick(const uint32_t *ws, EvictState st)
 {
     constexpr int PER = EV_BINS / EV_THREADS, NW = EV_THREADS / WAVE;
     static_assert(PER == 2, "the loads below");
@@ -176,10 +191,12 @@ __device__ __forceinline__ EvictState evict_pick(const uint32_t *hist_all, Evict
         return st;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-    const u32x2 *hist = (const u32x2 *)(hist_all + L * EV_COPIES * EV_BINS);
+    const u32x2 *hist =
+        (const u32x2 *)(ws + (L == 0 ? EV_AT_FIRST : EV_AT_HIST + (L - 1) * EV_HIST));
     u32x2 own = u32x2{0, 0};
-#pragma unroll
-    for (int k = 0; k < EV_COPIES; ++k)
+    const int copies = L == 0 && gridDim.x <= EV_OWN ? gridDim.x : EV_COPIES;
+#pragma unroll 8
+    for (int k = 0; k < copies; ++k)
         own += hist[k * (EV_BINS / 2) + tid];
     // rows in the bins of the threads before
     const uint32_t total = own[0] + own[1];
@@ -215,40 +232,78 @@ __device__ __forceinline__ EvictState evict_pick(const uint32_t *hist_all, Evict
 template <int L>
 __global__ __launch_bounds__(EV_THREADS) void evict_hist_kernel(const float *usage,
                                                                 const uint8_t *may_go, int N, int n,
-                                                                int rows, uint32_t *hist_all,
-                                                                EvictState *states)
+                                                                int rows, uint32_t *ws)
 {
     constexpr int SHIFT = ev_shift(L), BITS = ev_bits(L);
     constexpr uint32_t MASK = (1u << BITS) - 1;
-    __shared__ uint32_t bins[EV_BINS];
-    const int tid = threadIdx.x;
+    __shared__ uint32_t bins[EV_BINS], sums[EV_THREADS / WAVE], under;
+    EvictState *const states = (EvictState *)ws;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     for (int i = tid; i < EV_BINS; i += EV_THREADS)
         bins[i] = 0;
+    if (tid == 0)
+        under = 0;
+    if constexpr (L == 0)
+        for (int i = blockIdx.x * EV_THREADS + tid; i < 2 * EV_HIST; i += gridDim.x * EV_THREADS)
+            ws[EV_AT_HIST + i] = 0;
     EvictState st{0, (uint32_t)n, 0, 0};
     if constexpr (L > 0) {
         if constexpr (L > 1)
             st = states[L - 2];
-        st = evict_pick<L - 1>(hist_all, st);
+        st = evict_pick<L - 1>(ws, st);
         if (blockIdx.x == 0 && tid == 0)
             states[L - 1] = st;
-        if (st.all)
+        if (L < 2 && st.all)
             return;
     }
     __syncthreads();
     const long r0 = (long)blockIdx.x * rows;
+    uint32_t less = 0;   // the last histogram's: rows below all of its bins
 #pragma unroll 4
     for (int z = 0; z < rows; z += EV_TILE) {
         const Four f = load_four(usage, may_go, r0 + z + tid * 4, N);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (f.in[e] && (L == 0 || (f.key[e] >> (SHIFT + BITS)) == st.prefix))
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t high = L == 0 ? 0 : f.key[e] >> (SHIFT + BITS);
+            less += L == 2 && f.in[e] && (st.all || high < st.prefix);
+            if (f.in[e] && (L == 0 || (high == st.prefix && !st.all)))
                 atomicAdd(&bins[(f.key[e] >> SHIFT) & MASK], 1u);
+        }
+    }
+    if constexpr (L == 2) {
+        less = wave_reduce(less, [](uint32_t x, uint32_t y) { return x + y; });
+        if (lane == 0 && less)
+            atomicAdd(&under, less);
     }
     __syncthreads();
-    uint32_t *mine = hist_all + (L * EV_COPIES + blockIdx.x % EV_COPIES) * EV_BINS;
+    if (L == 0 && gridDim.x <= EV_OWN) {
+        for (int i = tid; i < EV_BINS; i += EV_THREADS)
+            ws[EV_AT_FIRST + blockIdx.x * EV_BINS + i] = bins[i];
+        return;
+    }
+    uint32_t *mine = ws + (L == 0 ? EV_AT_FIRST : EV_AT_HIST + (L - 1) * EV_HIST) +
+                     blockIdx.x % EV_COPIES * EV_BINS;
     for (int i = tid; i < EV_BINS; i += EV_THREADS)
         if (bins[i])
             atomicAdd(&mine[i], bins[i]);
+    if constexpr (L == 2) {
+        static_assert(EV_LAST == EV_THREADS && MASK + 1 == EV_LAST, "a bin a thread");
+        uint32_t upto = bins[tid];
+        for (int k = 1; k < WAVE; k <<= 1) {
+            const uint32_t x = (uint32_t)__shfl_up((int)upto, k);
+            upto += lane >= k ? x : 0;
+        }
+        if (lane == WAVE - 1)
+            sums[wave] = upto;
+        __syncthreads();
+        upto += under;
+        for (int w = 0; w < wave; ++w)
+            upto += sums[w];
+        uint32_t *cum = ws + EV_AT_CUM + (size_t)blockIdx.x * EV_CUM;
+        cum[tid + 1] = upto;
+        if (tid == 0)
+            cum[0] = under;
+    }
 }
 
 // A block's rows below T and at T.
@@ -283,60 +338,31 @@ __device__ __forceinline__ void block_sums(uint32_t &x, uint32_t &y,
     }
 }
 
-__global__ __launch_bounds__(EV_THREADS) void evict_count_kernel(const float *usage,
-                                                                 const uint8_t *may_go, int N,
-                                                                 int rows, const uint32_t *hist,
-                                                                 EvictState *states,
-                                                                 uint32_t *counts)
-{
-    __shared__ uint32_t red[2][EV_THREADS / WAVE];
-    const EvictState st = evict_pick<2>(hist, states[1]);
-    if (blockIdx.x == 0 && threadIdx.x == 0)
-        states[2] = st;
-    const uint32_t T = st.prefix;
-    const bool all = st.all != 0;
-    uint32_t below = 0, at = 0;
-    const long r0 = (long)blockIdx.x * rows;
-#pragma unroll 4
-    for (int z = 0; z < rows; z += EV_TILE) {
-        const Four f = load_four(usage, may_go, r0 + z + threadIdx.x * 4, N);
-        bool lt[4], eq[4];
-        below_and_at(f, T, all, lt, eq);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            below += lt[e];
-            at += eq[e];
-        }
-    }
-    block_sums(below, at, red);
-    if (threadIdx.x == 0) {
-        counts[blockIdx.x * 2] = below;
-        counts[blockIdx.x * 2 + 1] = at;
-    }
-}
-
 __global__ __launch_bounds__(EV_THREADS) void evict_write_kernel(const float *usage,
                                                                  const uint8_t *may_go, int N,
                                                                  int rows, int n,
-                                                                 const EvictState *st,
-                                                                 const uint32_t *counts,
+                                                                 const uint32_t *ws,
                                                                  int32_t *victims)
 {
     constexpr int NW = EV_THREADS / WAVE;
     __shared__ uint32_t red[2][NW];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const uint32_t T = st->prefix;   // (states[2])
-    const bool all = st->all != 0;
-    const uint32_t remain = all ? 0u : st->remain;
-    // rows below T and at T in the blocks before
-    uint32_t below = 0, at = 0;
-    for (int k = tid; k < (int)blockIdx.x; k += EV_THREADS) {
-        below += counts[2 * k];
-        at += counts[2 * k + 1];
-    }
+    const EvictState st = evict_pick<2>(ws, ((const EvictState *)ws)[1]);
+    const uint32_t T = st.prefix;
+    const bool all = st.all != 0;
+    const uint32_t remain = all ? 0u : st.remain;
+    // rows below T and at T, of a block
+    auto counts = [&](int k, uint32_t &b, uint32_t &a) {
+        const uint32_t *cum = ws + EV_AT_CUM + (size_t)k * EV_CUM + (all ? 0 : T & (EV_LAST - 1));
+        b = cum[0];
+        a = all ? 0u : cum[1] - cum[0];
+    };
+    uint32_t below = 0, at = 0, own_below, own_at;
+    if (tid < (int)blockIdx.x)
+        counts(tid, below, at);   // (of the blocks before)
+    counts(blockIdx.x, own_below, own_at);
     block_sums(below, at, red);
-    const bool none = counts[2 * blockIdx.x] == 0 &&
-                      (counts[2 * blockIdx.x + 1] == 0 || at >= remain);
+    const bool none = own_below == 0 && (own_at == 0 || at >= remain);
     const long r0 = (long)blockIdx.x * rows;
     if (!none) {
         const uint64_t under = (1ull << lane) - 1;
@@ -418,32 +444,28 @@ hipError_t launch_write_rows(int src_dtype, int dtype, const RowsArgs &a, hipStr
                                : write_rows<1>(dtype, a, (int)grid, s);
 }
 
-size_t evict_bytes(int)
+size_t evict_bytes(int N)
 {
-    return 256 + 3 * EV_COPIES * EV_BINS * 4 + EV_BLOCKS * 2 * 4;
+    const int rows = evict_rows(N);
+    return ((size_t)EV_AT_CUM + ((size_t)N + rows - 1) / rows * EV_CUM) * 4;
 }
 
 hipError_t launch_evict(const float *usage, const uint8_t *may_go, int N, int n, int32_t *victims,
-                        void *ws, hipStream_t s)
+                        void *ws_, hipStream_t s)
 {
-    EvictState *st = (EvictState *)ws;   // [3]
-    uint32_t *hist = (uint32_t *)((uint8_t *)ws + 256);
-    uint32_t *counts = hist + 3 * EV_COPIES * EV_BINS;
+    uint32_t *ws = (uint32_t *)ws_;
     const int rows = evict_rows(N);
-    const dim3 grid((unsigned)(((long)N + rows - 1) / rows)), block(EV_THREADS);
-    static_assert(3 * EV_COPIES * EV_BINS % EV_THREADS == 0, "the clearing grid");
-    hipLaunchKernelGGL(evict_clear_kernel, dim3(3 * EV_COPIES * EV_BINS / EV_THREADS), block, 0, s,
-                       hist);
-    hipLaunchKernelGGL(evict_hist_kernel<0>, grid, block, 0, s, usage, may_go, N, n, rows, hist,
-                       st);
-    hipLaunchKernelGGL(evict_hist_kernel<1>, grid, block, 0, s, usage, may_go, N, n, rows, hist,
-                       st);
-    hipLaunchKernelGGL(evict_hist_kernel<2>, grid, block, 0, s, usage, may_go, N, n, rows, hist,
-                       st);
-    hipLaunchKernelGGL(evict_count_kernel, grid, block, 0, s, usage, may_go, N, rows, hist, st,
-                       counts);
-    hipLaunchKernelGGL(evict_write_kernel, grid, block, 0, s, usage, may_go, N, rows, n, st + 2,
-                       counts, victims);
+    const int blocks = (int)(((long)N + rows - 1) / rows);
+    const dim3 grid((unsigned)blocks), block(EV_THREADS);
+    static_assert(EV_BLOCKS <= EV_THREADS, "a thread for each block before");
+    static_assert(EV_HIST % EV_THREADS == 0, "the clearing grid");
+    if (blocks > EV_OWN)
+        hipLaunchKernelGGL(evict_clear_kernel, dim3(EV_HIST / EV_THREADS), block, 0, s, ws);
+    hipLaunchKernelGGL(evict_hist_kernel<0>, grid, block, 0, s, usage, may_go, N, n, rows, ws);
+    hipLaunchKernelGGL(evict_hist_kernel<1>, grid, block, 0, s, usage, may_go, N, n, rows, ws);
+    hipLaunchKernelGGL(evict_hist_kernel<2>, grid, block, 0, s, usage, may_go, N, n, rows, ws);
+    hipLaunchKernelGGL(evict_write_kernel, grid, block, 0, s, usage, may_go, N, rows, n, ws,
+                       victims);
     return hipGetLastError();
 }
 
