@@ -43,9 +43,9 @@ struct AttendPlan {
 // Whether a batch goes by as a matrix product of tiles (attend_gemm.hpp) of 256
 // rows and 256 requests: more than half a tile of bf16 requests, for which the
 // scan by tiles of 64 would read the bank three times or more, and tiles for half
-// the compute units. Forward, scan / tiles: 256 x 100,000 x 768 97 /
-// 67 us, 512 x 100,000 x 384 95 / 83, but 128 x 100,000 x 768 59 / 67 and 150 x
-// 15,000 x 768 30 / 40.
+// the compute units. Forward, scan / tiles: 256 x 100,000 x 768 97 / 67 us, 512 x
+// 100,000 x 384 95 / 83, but 128 x 100,000 x 768 59 / 67 and 150 x 15,000 x 768 30 /
+// 40.
 inline bool at_gemm(int dtype, int B, int N, int d, int n_cu)
 {
     const long tiles = ((long)N + 255) / 256 * ((B + 255) / 256);

@@ -151,7 +151,8 @@ struct UsageArgs {
 
 // Weights of the bank's rows: as the forward pass, with the bank's rows over
 // the lanes, so that a row's sum over the requests is a sum over registers and
-// four lanes. There is no running maximum: lse is known.
+// four lanes. There is no running maximum: lse is known. Bound as that one: 64
+// requests over 100,000 x 768 bf16 30 us, 5.1 TB/s.
 template <int DT, int NG, int RT>
 __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_kernel(const UsageArgs A)
 {
@@ -226,7 +227,8 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_kernel(const UsageAr
 }
 
 // The same as a matrix product of tiles, for large bf16 batches; part [4 *
-// n_qt][N], one of the waves of each 64 requests.
+// n_qt][N], one of the waves of each 64 requests. 256 requests over 1,000,000 x 768:
+// 443 us, 890 TFLOP/s.
 __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_gemm_kernel(const UsageArgs A)
 {
     extern __shared__ __align__(16) uint8_t smem[];
@@ -528,7 +530,12 @@ __device__ __forceinline__ void load_dout(const DsArgs &A, int q0, int n, float 
 }
 
 // The pass by tiles of NG * 16 requests, as the forward one. TAB: their label
-// gradients are in LDS.
+// gradients are in LDS. 64 requests over 100,000 x 768 bf16 take 43 us, near the
+// bank's way from memory; 256 take 126, of which builds without the step in question
+// lay 45 to loading a row again for every 64 requests (16 rows x 64 bytes an
+// instruction, 22 bytes a clock and compute unit, whatever is in flight), 38 to what
+// follows the scores and 20 to storing ds. (Tiles of 256 x 256 through LDS, as in the
+// pass above, were no faster: nothing runs beside their longer ends.)
 template <int DT, int NG, bool TAB>
 __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void ds_kernel(const DsArgs A)
 {
