@@ -38,6 +38,15 @@ __device__ __forceinline__ size_t dout_place(int b, int c, int n_j)
     return ((size_t)(b >> 4) * n_j + (c >> 2)) * WAVE + (c & 3) * 16 + (b & 15);
 }
 
+// What rounding lse2 and c takes from the exponent of a row near the request (c * a
+// about lse2), of a request's weights as a whole: up to 2^-23 of lse2.
+__device__ __forceinline__ double lost_to_rounding(float lse, float lse2, double more)
+{
+    return lse == -INFINITY
+               ? 0.0
+               : more * (double)lse2 - ((double)lse * 1.4426950408889634 - (double)lse2);
+}
+
 template <int QDT>
 __device__ __forceinline__ void make_side(const PrepArgs &A, int b, int lane)
 {
@@ -56,12 +65,9 @@ __device__ __forceinline__ void make_side(const PrepArgs &A, int b, int lane)
     const float lse = A.lse[b];
     const bool alive = lse != -INFINITY;
     const float lse2 = alive ? lse * LOG2E : INFINITY;
-    // What rounding lse2 and c takes from the exponent of a row near the request
-    // (c * a about lse2), of a request's weights as a whole: up to 2^-23 of lse2.
-    // The gradients are linear in the weights, and get it with the outputs' ones;
-    // for the usage it goes into hq.
-    const double lost =
-        alive ? A.more * (double)lse2 - ((double)lse * 1.4426950408889634 - (double)lse2) : 0.0;
+    // (the gradients are linear in the weights, and get what rounding lost with the
+    // outputs' ones; for the usage it goes into hq)
+    const double lost = lost_to_rounding(lse, lse2, A.more);
     const float f = __builtin_amdgcn_exp2f((float)lost);
     double dot = 0.0;
     if (A.dout) {
@@ -142,7 +148,9 @@ __global__ __launch_bounds__(256) void prep_kernel(const PrepArgs A, int side_bl
 
 struct UsageArgs {
     AttendBank b;
-    const Side *side;
+    const float *lse;
+    double more;           // what c lacks, over c
+    const Side *side;      // of the pass by tiles
     int nks, n_chunks, n_qt;
     long slabs;
     float decay;
@@ -151,8 +159,9 @@ struct UsageArgs {
 
 // Weights of the bank's rows: as the forward pass, with the bank's rows over
 // the lanes, so that a row's sum over the requests is a sum over registers and
-// four lanes. There is no running maximum: lse is known. Bound as that one: 64
-// requests over 100,000 x 768 bf16 30 us, 5.1 TB/s.
+// four lanes. There is no running maximum: lse is known. The requests' norms come
+// from their tile in LDS (a launch before for them took 4.6 us). Bound as that one: 64
+// requests over 100,000 x 768 bf16 32 us, 4.8 TB/s.
 template <int DT, int NG, int RT>
 __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_kernel(const UsageArgs A)
 {
@@ -173,10 +182,24 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_kernel(const UsageAr
     const int N = A.b.N;
     const float c = A.b.c;
     load_requests<DT, NG>(A.b, A.nks, q0, qs, wave, n_waves, lane);
-    for (int i = tid; i < NG * 16; i += blockDim.x)
-        sd[i] = q0 + i < A.b.B ? A.side[q0 + i] : Side{0.f, INFINITY, 0.f, 0.f};
+    for (int i = tid; i < NG * 16; i += blockDim.x) {
+        const float lse = q0 + i < A.b.B ? A.lse[q0 + i] : -INFINITY;
+        const float lse2 = lse == -INFINITY ? INFINITY : lse * LOG2E;
+        sd[i] = Side{(float)(lost_to_rounding(lse, lse2, A.more) / c), lse2, 0.f, 0.f};
+    }
     float hq[NG][4], lse2[NG][4];
     auto ready = [&] {
+        for (int g = wave; g < NG; g += n_waves) {
+            double s = 0.0;
+#pragma unroll 4
+            for (int f = 0; f < A.nks * AtElem<DT>::SUB; ++f)
+                s += sumsq16<DT == AT_F32 ? 0 : 1>(qs[(f * NG + g) * WAVE + lane], 0.f);
+            s += __shfl_xor(s, 16);
+            s += __shfl_xor(s, 32);
+            if (jg == 0)
+                sd[g * 16 + col].hq = (float)((double)sd[g * 16 + col].hq - 0.5 * s);
+        }
+        stream_barrier();
 #pragma unroll
         for (int g = 0; g < NG; ++g)
 #pragma unroll
@@ -1351,7 +1374,7 @@ bool plan_usage(int B, int N, int d, int dtype, int n_cu, UsagePlan *p)
     p->nks = (d + ks - 1) / ks;
     p->gemm = at_gemm(dtype, B, N, d, n_cu);
     p->off_side = 0;
-    p->off_part = up256((size_t)B * sizeof(Side));
+    p->off_part = p->gemm ? up256((size_t)B * sizeof(Side)) : 0;
     const size_t group = (size_t)p->nks * ks * (dtype == AT_F32 ? 4 : 2) * 16 + 16 * sizeof(Side);
     if (p->gemm) {
         p->nks = (d + AG_K - 1) / AG_K;
@@ -1374,7 +1397,8 @@ bool plan_usage(int B, int N, int d, int dtype, int n_cu, UsagePlan *p)
     shares(p->slabs, slab, dtype, d, p->n_qt, n_cu, &p->n_chunks, &p->waves);
     p->lds_bytes = group * ng;
     p->n_part = p->n_qt;
-    p->bytes = p->off_part + (p->n_qt > 1 ? up256((size_t)p->n_qt * N * 4) : 0);
+    // (256 bytes where nothing is needed: a workspace is asked for all the same)
+    p->bytes = p->off_part + (p->n_qt > 1 ? up256((size_t)p->n_qt * N * 4) : 256);
     return true;
 }
 
@@ -1382,19 +1406,24 @@ hipError_t launch_usage(const UsagePlan &p, const AttendBank &b, const float *ls
                         float *usage, void *ws, hipStream_t s)
 {
     Side *side = (Side *)((uint8_t *)ws + p.off_side);
-    PrepArgs pa{};
-    pa.queries = b.queries;
-    pa.B = pa.places = b.B;
-    pa.d = b.d;
-    pa.lse = lse;
-    pa.side = side;
-    pa.c = b.c;
-    pa.more = b.c_exact() / b.c - 1.0;
-    hipError_t e = p.dtype == AT_F32 ? run_prep<0>(pa, s) : run_prep<1>(pa, s);
-    if (e != hipSuccess)
-        return e;
+    const double more = b.c_exact() / b.c - 1.0;
+    hipError_t e = hipSuccess;
+    if (p.gemm) {
+        PrepArgs pa{};
+        pa.queries = b.queries;
+        pa.B = pa.places = b.B;
+        pa.d = b.d;
+        pa.lse = lse;
+        pa.side = side;
+        pa.c = b.c;
+        pa.more = more;
+        if ((e = run_prep<1>(pa, s)) != hipSuccess)
+            return e;
+    }
     UsageArgs a;
     a.b = b;
+    a.lse = lse;
+    a.more = more;
     a.side = side;
     a.nks = p.nks;
     a.n_chunks = p.n_chunks;
