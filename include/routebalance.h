@@ -398,7 +398,7 @@ rb_status rb_route_batch_noalloc(const void *queries, const void *bank, const fl
  * enqueues nothing but (rb_attend_usage) the decay and (rb_attend_backward) the
  * zeros of the gradients of the bank.
  * Scores 2*beta*<q, x> and beta*|x|^2 must stay within fp32 (below 3e38).
- * Errors shared by the calls: RB_ERR_DTYPE; RB_ERR_DIMS (B < 0, B >= 2^24, N < 1, d < 1,
+ * Errors shared by the calls: RB_ERR_DTYPE; RB_ERR_DIMS (B < 0, B >= 2^23, N < 1, d < 1,
  * d > RB_MAX_D, d not a multiple of 4 for RB_F32, 8 for RB_BF16, 32 for RB_Q4,
  * M < 1, M > RB_MAX_M); RB_ERR_VALUE; RB_ERR_NULL; RB_ERR_ALIGN; RB_ERR_WORKSPACE;
  * RB_ERR_HIP. The *_workspace_size calls write the bytes for these sizes on the

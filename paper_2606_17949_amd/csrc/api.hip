@@ -279,7 +279,7 @@ rb_status route_batch(const void *queries, const void *bank, const float *bank_n
     return hip_status(e);
 }
 
-constexpr int MAX_B = (1 << 24) - 1;   // (a grid holds 2^32 threads: 256 join a request's parts)
+constexpr int MAX_B = (1 << 23) - 1;   // (a grid holds 2^32 threads: 256 a request join its parts)
 
 // Sizes of a bank that may also be held in 4 bits.
 rb_status check_attend_dims(rb_dtype dt, int B, int N, int d)

@@ -1099,31 +1099,65 @@ __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
         }
 }
 
-// d_queries and d_beta: the shares' sums, 2 beta (sum - q * sum of ds). One
-// workgroup per request and 256 columns, a wave every fourth share.
+struct JoinArgs {
+    // d_queries and d_beta (null: not wanted)
+    const float *part, *req;
+    int n_part, n_req, B, d;
+    const uint8_t *queries;
+    float scale;
+    uint8_t *d_queries;
+    float *d_beta;
+    int n_dq, n_col;             // workgroups of these, for the columns of a request
+    // the label gradients of several request tiles, [n_qt][n] each
+    const float *lab[2];
+    float *out[2];               // null: not wanted
+    int n_qt;
+    size_t n;
+};
+
+// The request tiles' label gradients, added in order.
+__device__ __forceinline__ void join_labels(const JoinArgs &A, int block, int blocks)
+{
+    for (int h = 0; h < 2; ++h) {
+        if (!A.out[h])
+            continue;
+        for (size_t i = (size_t)block * 256 + threadIdx.x; i < A.n; i += (size_t)blocks * 256) {
+            float s = 0.f;
+#pragma unroll 4
+            for (int t = 0; t < A.n_qt; ++t)
+                s += A.lab[h][(size_t)t * A.n + i];
+            A.out[h][i] = s;
+        }
+    }
+}
+
+// What shares and request tiles left, joined. d_queries and d_beta: the shares'
+// sums, 2 beta (sum - q * sum of ds); a workgroup per request and 256 columns, a
+// wave every fourth share. The label gradients: the workgroups behind them.
 template <int DT>
-__global__ __launch_bounds__(256) void dq_join_kernel(const float *part, int n_part,
-                                                      const float *req, int n_req,
-                                                      const uint8_t *queries, int B, int d,
-                                                      float scale, uint8_t *d_queries,
-                                                      float *d_beta)
+__global__ __launch_bounds__(256) void grad_join_kernel(const JoinArgs A)
 {
     __shared__ float red[2][4];
     __shared__ f32x4 sums[3][WAVE];
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int c0 = blockIdx.y * 256 + lane * 4;
-    const bool in = d_queries && c0 < d;
+    if ((int)blockIdx.x >= A.n_dq) {
+        join_labels(A, blockIdx.x - A.n_dq, gridDim.x - A.n_dq);
+        return;
+    }
+    const int b = blockIdx.x / A.n_col, y = blockIdx.x % A.n_col;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int c0 = y * 256 + lane * 4;
+    const bool in = A.d_queries && c0 < A.d;
     f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
     if (in) {
-        const float *at = part + (size_t)b * d + c0;
-        const size_t step = (size_t)B * d;
+        const float *at = A.part + (size_t)b * A.d + c0;
+        const size_t step = (size_t)A.B * A.d;
 #pragma unroll 8
-        for (int k = wave; k < n_part; k += 4)
+        for (int k = wave; k < A.n_part; k += 4)
             v += *(const f32x4 *)(at + k * step);
     }
     float s0 = 0.f, s1 = 0.f;
-    for (int k = tid; k < n_req; k += 256) {
-        const float *at = req + ((size_t)k * B + b) * 2;
+    for (int k = tid; k < A.n_req; k += 256) {
+        const float *at = A.req + ((size_t)k * A.B + b) * 2;
         s0 += at[0];
         s1 += at[1];
     }
@@ -1136,34 +1170,18 @@ __global__ __launch_bounds__(256) void dq_join_kernel(const float *part, int n_p
     if (wave > 0)
         sums[wave - 1][lane] = v;
     __syncthreads();
-    if (tid == 0 && blockIdx.y == 0 && d_beta)
-        d_beta[b] = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+    if (tid == 0 && y == 0 && A.d_beta)
+        A.d_beta[b] = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
     if (wave > 0 || !in)
         return;
     const float sum = (red[0][0] + red[0][1]) + (red[0][2] + red[0][3]);
     for (int w = 0; w < 3; ++w)
         v += sums[w][lane];
-    const f32x4 q = load4<DT>(queries, (size_t)b * d + c0);
+    const f32x4 q = load4<DT>(A.queries, (size_t)b * A.d + c0);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-        v[e] = scale * (v[e] - q[e] * sum);
-    store4<DT>(d_queries, (size_t)b * d + c0, v);
-}
-
-// The request tiles' label gradients, added in order (grid.y: one or both kinds).
-__global__ __launch_bounds__(256) void label_join_kernel(const float *part0, float *out0,
-                                                         const float *part1, float *out1, int n_qt,
-                                                         size_t n)
-{
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-    const float *part = blockIdx.y ? part1 : part0;
-    float *out = blockIdx.y ? out1 : out0;
-    if (i >= n || !out)
-        return;
-    float s = 0.f;
-    for (int t = 0; t < n_qt; ++t)
-        s += part[(size_t)t * n + i];
-    out[i] = s;
+        v[e] = A.scale * (v[e] - q[e] * sum);
+    store4<DT>(A.d_queries, (size_t)b * A.d + c0, v);
 }
 
 template <typename K>
@@ -1347,22 +1365,34 @@ hipError_t run_grad(const GradPlan &p, const AttendBank &b, const GradArgs &g, u
                 return e;
         }
     }
-    if (g.d_queries || g.d_beta) {
-        hipLaunchKernelGGL(dq_join_kernel<DT>,
-                           dim3(b.B, g.d_queries ? (b.d + 255) / 256 : 1), dim3(256), 0, s, dq,
-                           p.q_chunks, a.req, p.n_chunks, b.queries, b.B, b.d, scale,
-                           (uint8_t *)g.d_queries, g.d_beta);
-        if ((e = hipGetLastError()) != hipSuccess)
-            return e;
-    }
+    JoinArgs w{};
+    w.part = dq;
+    w.req = a.req;
+    w.n_part = p.q_chunks;
+    w.n_req = p.n_chunks;
+    w.B = b.B;
+    w.d = b.d;
+    w.queries = b.queries;
+    w.scale = scale;
+    w.d_queries = (uint8_t *)g.d_queries;
+    w.d_beta = g.d_beta;
+    w.n_col = g.d_queries ? (b.d + 255) / 256 : 1;
+    w.n_dq = g.d_queries || g.d_beta ? b.B * w.n_col : 0;
+    size_t blocks = 0;
     if (p.n_qt > 1) {
+        w.lab[0] = a.d_qual;
+        w.lab[1] = a.d_len;
+        w.out[0] = g.d_qual;
+        w.out[1] = g.d_len;
+        w.n_qt = p.n_qt;
+        w.n = n_lab;
         if (g.d_qual || g.d_len)
-            hipLaunchKernelGGL(label_join_kernel, dim3((unsigned)((n_lab + 255) / 256), 2),
-                               dim3(256), 0, s, a.d_qual, g.d_qual, a.d_len, g.d_len, p.n_qt,
-                               n_lab);
-        e = hipGetLastError();
+            blocks = (n_lab + 255) / 256 < 8192 ? (n_lab + 255) / 256 : 8192;
     }
-    return e;
+    if (w.n_dq + blocks == 0)
+        return hipSuccess;
+    hipLaunchKernelGGL(grad_join_kernel<DT>, dim3((unsigned)(w.n_dq + blocks)), dim3(256), 0, s, w);
+    return hipGetLastError();
 }
 
 }  // namespace

@@ -32,7 +32,7 @@ def usage(q=FAKE, x=FAKE, sc=None, norms=FAKE, dt=rb.RB_BF16, B=4, N=100, d=64, 
 
 
 SIZES = [(dict(B=-1), rb.RB_ERR_DIMS), (dict(N=0), rb.RB_ERR_DIMS), (dict(d=0), rb.RB_ERR_DIMS),
-         (dict(B=1 << 24), rb.RB_ERR_DIMS),
+         (dict(B=1 << 23), rb.RB_ERR_DIMS),
          (dict(d=60), rb.RB_ERR_DIMS), (dict(d=2056), rb.RB_ERR_DIMS),
          (dict(dt=rb.RB_F32, d=6), rb.RB_ERR_DIMS), (dict(dt=7), rb.RB_ERR_DTYPE),
          (dict(dt=-1), rb.RB_ERR_DTYPE), (dict(beta=0.0), rb.RB_ERR_VALUE),
