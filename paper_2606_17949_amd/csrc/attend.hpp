@@ -35,7 +35,7 @@ struct AttendPlan {
     int waves, nks;        // waves of a workgroup, k-steps of a row
     int n_lt;              // tiles of label columns
     int ct;                //   of ct * 16 columns each
-    int slabs;             // pieces of 32 rows
+    int slabs;             // pieces of the bank: slabs, or tiles of 256 rows
     size_t lds_bytes;
     size_t off_ml, off_o, bytes;   // workspace: partial maxima and sums, partial averages
 };
