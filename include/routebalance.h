@@ -469,7 +469,8 @@ rb_status rb_bank_pack(const void *bank, rb_dtype dtype, int N, int d, uint8_t *
                        uint8_t *scales, float *norms, void *stream);
 
 /* Rows to make room: the n rows of least usage among those whose may_go is not 0
- * (NULL: all), equal usage (0 and -0 are equal) by the lower row first, NaN last.
+ * (NULL: all), equal usage (0 and -0 are equal) by the lower row first, NaN of either
+ * sign last (among them the lower row first).
  *   usage [N] fp32; may_go [N] uint8 or NULL; victims [n] int32 (output): row
  *   indices ascending, -1 behind them if fewer than n rows may go.
  * n = 0 enqueues nothing. Errors: RB_ERR_DIMS (N < 1, n < 0, n > N), RB_ERR_NULL,

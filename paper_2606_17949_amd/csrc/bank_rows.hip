@@ -139,7 +139,12 @@ struct EvictState {
     uint32_t prefix, remain, all, none;
 };
 
-__device__ __forceinline__ uint32_t usage_key(float u) { return f2key(u + 0.f); }   // -0 is 0
+// Ordered bits of a usage: -0 is 0, and every NaN, of either sign, the greatest key
+// (f2key orders numbers only: a NaN with the sign bit set comes below -inf there).
+__device__ __forceinline__ uint32_t usage_key(float u)
+{
+    return u != u ? KEY_NONE : f2key(u + 0.f);
+}
 
 // Rows i .. i+3: their keys, and which of them may go (none past the end).
 struct Four {
