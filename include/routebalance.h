@@ -410,6 +410,10 @@ rb_status rb_route_batch_noalloc(const void *queries, const void *bank, const fl
  *   bank_qual, bank_len [N][M] fp32; q_hat, l_hat [B][M] fp32 (outputs);
  *   lse [B] fp32 (output, may be NULL). The outputs can go to rb_score and
  *   rb_assign as those of rb_knn_predict do.
+ *   Labels of rows that are not masked are below 1e30 in magnitude, or are no
+ *   numbers: one that is NaN makes its model's predictions NaN, an infinite one
+ *   infinite (NaN where a weight falls below 1e-38 of the largest, or where both
+ *   infinities meet).
  * Sums, maxima and weights are fp32. */
 rb_status rb_attend_workspace_size(int B, int N, int d, rb_dtype dtype, int M, size_t *bytes);
 rb_status rb_attend(const void *queries, const void *bank, const uint8_t *scales,

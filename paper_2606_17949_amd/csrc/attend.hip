@@ -255,6 +255,9 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
     };
 
     float ref[AG_NG], sub[AG_NG];
+    // of the lane's label column, the sum of the labels that are no numbers: every
+    // weight is above 0, so a request's average is that sum whatever its weights
+    float beyond = 0.f;
     f32x4 o[AG_NG], ol[ONES ? AG_NG : 1];
 #pragma unroll
     for (int g = 0; g < AG_NG; ++g) {
@@ -303,12 +306,13 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
                     ol[g] *= f;
             }
         }
+        uint32_t odd = 0;   // the largest of the labels' magnitudes, doubled
         const i32x4 ones = i32x4{ONE2, ONE2, ONE2, ONE2};
 #pragma unroll
         for (int r = 0; r < AG_RT; r += 2) {
             __builtin_amdgcn_sched_barrier(0);
-            // the labels of these 32 rows as three bf16 values each (those of rows
-            // without weight may be no numbers: made finite)
+            // the labels of these 32 rows as three bf16 values each, made finite (those
+            // of rows without weight may hold anything)
             i32x4 vh, vm, vl;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -317,6 +321,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
                 for (int i = 0; i < 2; ++i) {
                     const float y = labels[(8 * (4 * wr + r / 2) + 2 * j + i) * WAVE + lane];
                     x[i] = one ? 1.f : __builtin_amdgcn_fmed3f(y, -3e38f, 3e38f);
+                    odd = max(odd, __float_as_uint(y) << 1);
                 }
                 vh[j] = split_bf16(x[0], x[1]);
                 vm[j] = split_bf16(x[0], x[1]);
@@ -357,6 +362,16 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
             }
         }
         __builtin_amdgcn_sched_barrier(0);
+        // labels that are no numbers, in rows that are not masked
+        if (ballot(odd >= 0xff000000u))
+#pragma unroll 1
+            for (int k = 0; k < 32; ++k) {
+                const float y = labels[(32 * wr + k) * WAVE + lane];
+                const int at = 128 * wr + 32 * (k >> 3) + 16 * (k >> 2 & 1) + 4 * jg + (k & 3);
+                if (!__builtin_isfinite(y) && tile_norm(A.b, side, left, at) != -INFINITY)
+                    beyond += y;
+            }
+        __builtin_amdgcn_sched_barrier(0);
     };
     gemm_tiles<false, 8>(A.b, A.nks, ring, side, labels, q0, t0, (int)(t1 - t0), wave, lane,
                              label, end);
@@ -364,8 +379,12 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
     // ---- the two halves of the rows joined: maximum, then 16 columns (and the
     // sum of the weights, where it is none of them)
     constexpr int W = 18;
-    float *jn = (float *)smem;   // [2][256][W]
+    float *jn = (float *)smem;            // [2][256][W]
+    float *far = jn + 2 * AG_REQS * W;    // [2][16]
     stream_barrier();
+    beyond = rows_reduce(cc < 2 * M ? beyond : 0.f, [](float x, float y) { return x + y; });
+    if (wq == 0 && jg == 0)
+        far[16 * wr + col] = beyond;
 #pragma unroll
     for (int g = 0; g < AG_NG; ++g) {
         float *at = jn + (wr * AG_REQS + 64 * wq + 16 * g + col) * W;
@@ -394,7 +413,8 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
         if (b[0] != -INFINITY)
             sum = fmaf(__builtin_amdgcn_exp2f(b[0] - m), b[1 + x], sum);
         if (x > 0) {
-            A.o[(((size_t)ch * gridDim.y + lt) * A.b.B + q0 + q) * 16 + x - 1] = sum;
+            A.o[(((size_t)ch * gridDim.y + lt) * A.b.B + q0 + q) * 16 + x - 1] =
+                sum + (far[x - 1] + far[15 + x]);
         } else if (lt == 0) {
             float *ml = A.ml + ((size_t)ch * A.b.B + q0 + q) * 2;
             ml[0] = m;
