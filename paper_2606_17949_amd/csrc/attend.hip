@@ -11,6 +11,14 @@ namespace {
 // two: weights stay below 2^16 and few slabs rescale what went before.
 constexpr float AT_SLACK = 16.f;
 
+// What the sums of a part of the rows, relative to its maximum, count for beside
+// the whole's maximum m. A part without one has no rows with weight, whose sums are
+// 0, or rows whose scores are no numbers, whose sums are none either and have to show.
+__device__ __forceinline__ float part_weight(float part, float m)
+{
+    return part == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(part - m);
+}
+
 struct AttendArgs {
     AttendBank b;
     const float *qual, *len;
@@ -200,8 +208,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
             m = fmaxf(m, jn[(w * NG * 16 + q) * W]);
         for (int w = 0; w < n_waves; ++w) {
             const float *at = jn + (w * NG * 16 + q) * W;
-            if (at[0] != -INFINITY)
-                sum = fmaf(__builtin_amdgcn_exp2f(at[0] - m), at[1 + x], sum);
+            sum = fmaf(part_weight(at[0], m), at[1 + x], sum);
         }
         if (x > 0) {
             A.o[(((size_t)ch * gridDim.y + lt) * A.b.B + q0 + q) * (16 * CT) + x - 1] = sum;
@@ -407,11 +414,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
             continue;
         const float *a = jn + q * W, *b = a + AG_REQS * W;
         const float m = fmaxf(a[0], b[0]);
-        float sum = 0.f;
-        if (a[0] != -INFINITY)
-            sum = __builtin_amdgcn_exp2f(a[0] - m) * a[1 + x];
-        if (b[0] != -INFINITY)
-            sum = fmaf(__builtin_amdgcn_exp2f(b[0] - m), b[1 + x], sum);
+        const float sum = fmaf(part_weight(b[0], m), b[1 + x], part_weight(a[0], m) * a[1 + x]);
         if (x > 0) {
             A.o[(((size_t)ch * gridDim.y + lt) * A.b.B + q0 + q) * 16 + x - 1] =
                 sum + (far[x - 1] + far[15 + x]);
@@ -476,9 +479,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const float *ml, const
     for (int ch = tid + 256; ch < n_chunks; ch += 256)
         m = fmaxf(m, pair(ch)[0]);
     m = over(0, m, [](float u, float v) { return fmaxf(u, v); }, -INFINITY);
-    auto weight = [&](float v) {
-        return v == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(v - m);
-    };
+    auto weight = [&](float v) { return part_weight(v, m); };
     float sum = weight(mine[0]) * mine[1];
     wts[tid] = weight(mine[0]);
     for (int ch = tid + 256; ch < n_chunks; ch += 256) {

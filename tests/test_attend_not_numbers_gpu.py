@@ -1,4 +1,4 @@
-"""Labels and requests that are no numbers and are not masked (GPU): they
+"""Labels, rows and requests that are no numbers and are not masked (GPU): they
 show in the predictions that they enter, and in no others, alike for every type
 and size of batch."""
 import math
@@ -43,6 +43,24 @@ def test_labels_that_are_no_numbers(dtype, B, N, M, masked):
     for k in want:
         assert torch.equal(torch.nan_to_num(got[k], 7.5, 1e38, -1e38),
                            torch.nan_to_num(want[k], 7.5, 1e38, -1e38)), k
+
+
+@pytest.mark.parametrize("which", ["all", "first tile", "half a tile", "one"])
+@pytest.mark.parametrize("B,N", BATCHES)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "q4"])
+def test_rows_that_are_no_numbers(dtype, B, N, which):
+    """One distance that is no number makes the softmax none, also where a wave or
+    a tile has no other rows."""
+    s = make(dtype, B, N, 128, 3)
+    rows = {"all": slice(0, N), "first tile": slice(0, 256), "half a tile": slice(128, 256),
+            "one": slice(N - 1, N)}[which]
+    s["norms"][rows] = math.nan
+    if dtype != "q4":
+        s["bank"][rows] = math.nan
+    out = forward(s, 4.0)
+    torch.cuda.synchronize()
+    for k, v in out.items():
+        assert torch.isnan(v).all(), k
 
 
 @pytest.mark.parametrize("B,N", BATCHES)
