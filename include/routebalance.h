@@ -379,8 +379,10 @@ rb_status rb_route_batch_noalloc(const void *queries, const void *bank, const fl
  * (a softmax over the negated squared distances, j over the rows whose mask is
  * not 0), which is smooth in the requests, the rows, the labels and beta, so that
  * all four can be trained. Distances as in rb_knn_topk (fp32 products and
- * accumulation); the maximum of the softmax is subtracted, so no weight
- * overflows. Arguments shared by the calls:
+ * accumulation): one is off by about (|q|^2 + |x|^2) * 2^-23, and a weight by a
+ * factor of e to beta times that. rb_attend subtracts the largest score before
+ * beta multiplies: the nearest row's weight is the largest, and a number, at any
+ * beta. Arguments shared by the calls:
  *   queries   [B][d] of dtype (bf16 for RB_Q4), 16-byte aligned.
  *   bank      RB_F32, RB_BF16: [N][d]; RB_Q4: [N][d/2] bytes (rb_bank_pack);
  *             16-byte aligned.

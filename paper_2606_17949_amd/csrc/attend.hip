@@ -9,14 +9,23 @@ namespace {
 
 // A running maximum is raised when a score passes it by this many powers of
 // two: weights stay below 2^16 and few slabs rescale what went before.
+// The maximum is kept in units of the scores and subtracted before c multiplies: the
+// largest weight is then 1 (2^AT_SLACK at most) for any c. (Subtracted from rounded
+// products c*u, it left up to half a step of them in the exponent: from c*u = 2^31 on
+// weights of 0 or infinity.)
 constexpr float AT_SLACK = 16.f;
 
+// The maximum of no scores: below any, and a number, so that differences are none
+// that is not. What has only masked rows keeps it, with sums of 0, and so does what
+// has only rows whose scores are no numbers, with sums that are none and show
+// whatever weight they are joined with.
+constexpr float AT_NO_MAX = -3.402823466e38f;
+
 // What the sums of a part of the rows, relative to its maximum, count for beside
-// the whole's maximum m. A part without one has no rows with weight, whose sums are
-// 0, or rows whose scores are no numbers, whose sums are none either and have to show.
-__device__ __forceinline__ float part_weight(float part, float m)
+// the whole's maximum m.
+__device__ __forceinline__ float part_weight(float c, float part, float m)
 {
-    return part == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(part - m);
+    return __builtin_amdgcn_exp2f(c * (part - m));
 }
 
 struct AttendArgs {
@@ -24,17 +33,17 @@ struct AttendArgs {
     const float *qual, *len;
     int M, nks, n_chunks, n_qt;
     long slabs;
-    float *ml;   // [n_chunks][B][2] maximum (of t) and sum of the weights
+    float *ml;   // [n_chunks][B][2] maximum (of u) and sum of the weights
     float *o;    // [n_chunks][n_lt][B][ct * 16] sums of weighted labels
 };
 
 // One workgroup per (share of the bank, tile of NG * 16 requests, tile of CT *
 // 16 label columns); each wave has its own part of the share, its own running
 // maximum and sums, and the waves' are joined in LDS at the end.
-//   scores   u = <q, x> - |x|^2/2 (MFMA), t = c*u (|q|^2 changes no weight; the
-//            join adds it to lse)
-//   maximum  raised now and then, the sums rescaled when it is
-//   weights  p = 2^(t - maximum), their sum, and sum of p * label as a second
+//   scores   u = <q, x> - |x|^2/2 (MFMA; |q|^2 changes no weight; the join adds it
+//            to lse)
+//   maximum  of u, raised now and then, the sums rescaled when it is
+//   weights  p = 2^(c * (u - maximum)), their sum, and sum of p * label as a second
 //            MFMA (fp32, 16 label columns x 16 requests, 4 rows): its operand
 //            p[row 4*(lane/16) + e][request lane%16] is register e of the
 //            scores as it stands.
@@ -72,12 +81,11 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
         lab_ok[k] = cc < 2 * A.M;
         lab[k] = cc < A.M ? A.qual + cc : lab_ok[k] ? A.len + (cc - A.M) : A.qual;
     }
-    float ref[NG], sub[NG], l[NG];
+    float ref[NG], l[NG];
     f32x4 o[NG][CT];
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-        ref[g] = -INFINITY;   // the maximum that the sums are relative to
-        sub[g] = 0.f;         // the same, 0 where there is none yet
+        ref[g] = AT_NO_MAX;   // the maximum that the sums are relative to
         l[g] = 0.f;
 #pragma unroll
         for (int k = 0; k < CT; ++k)
@@ -140,7 +148,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
 #pragma unroll
             for (int r = 0; r < RT; ++r)
                 m = fmaxf(m, max4(acc[r][g]));
-            raise |= c * m > ref[g] + AT_SLACK;
+            raise |= c * (m - ref[g]) > AT_SLACK;
         }
         if (ballot(raise)) {
 #pragma unroll
@@ -149,11 +157,10 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
 #pragma unroll
                 for (int r = 0; r < RT; ++r)
                     m = fmaxf(m, max4(acc[r][g]));
-                m = rows_reduce(c * m, [](float x, float y) { return fmaxf(x, y); });
+                m = rows_reduce(m, [](float x, float y) { return fmaxf(x, y); });
                 const float up = fmaxf(ref[g], m);
-                const float f = ref[g] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[g] - up);
+                const float f = part_weight(c, ref[g], up);
                 ref[g] = up;
-                sub[g] = up == -INFINITY ? 0.f : up;
                 l[g] *= f;
 #pragma unroll
                 for (int k = 0; k < CT; ++k)
@@ -168,7 +175,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(c, acc[r][g][e], -sub[g]));
+                    const float p = __builtin_amdgcn_exp2f(c * (acc[r][g][e] - ref[g]));
                     l[g] += p;
 #pragma unroll
                     for (int k = 0; k < CT; ++k)
@@ -203,12 +210,12 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
         const int q = i / (W - 1), x = i - q * (W - 1);   // x 0: the sum, else a column
         if (q0 + q >= A.b.B)
             continue;
-        float m = -INFINITY, sum = 0.f;
+        float m = AT_NO_MAX, sum = 0.f;
         for (int w = 0; w < n_waves; ++w)
             m = fmaxf(m, jn[(w * NG * 16 + q) * W]);
         for (int w = 0; w < n_waves; ++w) {
             const float *at = jn + (w * NG * 16 + q) * W;
-            sum = fmaf(part_weight(at[0], m), at[1 + x], sum);
+            sum = fmaf(part_weight(c, at[0], m), at[1 + x], sum);
         }
         if (x > 0) {
             A.o[(((size_t)ch * gridDim.y + lt) * A.b.B + q0 + q) * (16 * CT) + x - 1] = sum;
@@ -261,15 +268,14 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
         return lab + (size_t)min(row, (long)N - 1) * M;
     };
 
-    float ref[AG_NG], sub[AG_NG];
+    float ref[AG_NG];
     // of the lane's label column, the sum of the labels that are no numbers: every
     // weight is above 0, so a request's average is that sum whatever its weights
     float beyond = 0.f;
     f32x4 o[AG_NG], ol[ONES ? AG_NG : 1];
 #pragma unroll
     for (int g = 0; g < AG_NG; ++g) {
-        ref[g] = -INFINITY;
-        sub[g] = 0.f;
+        ref[g] = AT_NO_MAX;
         o[g] = f32x4{0.f, 0.f, 0.f, 0.f};
         ol[ONES ? g : 0] = o[g];
     }
@@ -298,16 +304,15 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
         }
 #pragma unroll
         for (int g = 0; g < AG_NG; ++g)
-            raise |= c * top[g] > ref[g] + AT_SLACK;
+            raise |= c * (top[g] - ref[g]) > AT_SLACK;
         if (ballot(raise)) {
 #pragma unroll
             for (int g = 0; g < AG_NG; ++g) {
                 const float m =
-                    rows_reduce(c * top[g], [](float x, float y) { return fmaxf(x, y); });
+                    rows_reduce(top[g], [](float x, float y) { return fmaxf(x, y); });
                 const float up = fmaxf(ref[g], m);
-                const float f = ref[g] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[g] - up);
+                const float f = part_weight(c, ref[g], up);
                 ref[g] = up;
-                sub[g] = up == -INFINITY ? 0.f : up;
                 o[g] *= f;
                 if constexpr (ONES)
                     ol[g] *= f;
@@ -342,8 +347,8 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const f32x4 &u = acc[r + (j >> 1)][g];
-                    float x = __builtin_amdgcn_exp2f(fmaf(c, u[2 * (j & 1)], -sub[g]));
-                    float y = __builtin_amdgcn_exp2f(fmaf(c, u[2 * (j & 1) + 1], -sub[g]));
+                    float x = __builtin_amdgcn_exp2f(c * (u[2 * (j & 1)] - ref[g]));
+                    float y = __builtin_amdgcn_exp2f(c * (u[2 * (j & 1) + 1] - ref[g]));
                     ph[g][j] = split_bf16(x, y);
                     pl[g][j] = split_bf16(x, y);
                 }
@@ -414,7 +419,8 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
             continue;
         const float *a = jn + q * W, *b = a + AG_REQS * W;
         const float m = fmaxf(a[0], b[0]);
-        const float sum = fmaf(part_weight(b[0], m), b[1 + x], part_weight(a[0], m) * a[1 + x]);
+        const float sum =
+            fmaf(part_weight(c, b[0], m), b[1 + x], part_weight(c, a[0], m) * a[1 + x]);
         if (x > 0) {
             A.o[(((size_t)ch * gridDim.y + lt) * A.b.B + q0 + q) * 16 + x - 1] =
                 sum + (far[x - 1] + far[15 + x]);
@@ -433,7 +439,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_gemm_kernel(const A
 __global__ __launch_bounds__(256) void attend_join_kernel(const float *ml, const float *o,
                                                           int n_chunks, int n_lt, int width, int B,
                                                           int M, const uint8_t *queries, int qbytes,
-                                                          bool bf16, double c, double more,
+                                                          bool bf16, float c, double c_exact,
                                                           float *q_hat, float *l_hat, float *lse)
 {
     __shared__ float red[256], wts[256], part[2][4];
@@ -453,7 +459,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const float *ml, const
     };
     auto pair = [&](int ch) {
         return ch < n_chunks ? *(const f32x2 *)(ml + ((size_t)ch * B + b) * 2)
-                             : f32x2{-INFINITY, 0.f};
+                             : f32x2{AT_NO_MAX, 0.f};
     };
     // column cc of 16 of the 256 shares from k0 on
     auto columns = [&](int c0, int k0, float(&x)[16]) {
@@ -478,8 +484,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const float *ml, const
     float m = mine[0];
     for (int ch = tid + 256; ch < n_chunks; ch += 256)
         m = fmaxf(m, pair(ch)[0]);
-    m = over(0, m, [](float u, float v) { return fmaxf(u, v); }, -INFINITY);
-    auto weight = [&](float v) { return part_weight(v, m); };
+    m = over(0, m, [](float u, float v) { return fmaxf(u, v); }, AT_NO_MAX);
+    auto weight = [&](float v) { return part_weight(c, v, m); };
     float sum = weight(mine[0]) * mine[1];
     wts[tid] = weight(mine[0]);
     for (int ch = tid + 256; ch < n_chunks; ch += 256) {
@@ -488,15 +494,14 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const float *ml, const
     }
     const float total = over(1, sum, [](float u, float v) { return u + v; }, 0.f);
     if (lse) {
-        // the maximum and c*|q|^2/2 nearly cancel: in 64 bits, with what rounding c
-        // took from them
+        // the maximum and |q|^2/2 nearly cancel: in 64 bits, with c unrounded
         const double w2 = wave_sum64(q2);
         if ((tid & 63) == 0)
             squares[wave] = w2;
         __syncthreads();
         if (tid == 0) {
             const double s2 = (squares[0] + squares[1]) + (squares[2] + squares[3]);
-            lse[b] = (float)(((m - 0.5 * c * s2) * more + __builtin_amdgcn_logf(total)) *
+            lse[b] = (float)(((m - 0.5 * s2) * c_exact + __builtin_amdgcn_logf(total)) *
                              0.6931471805599453);
         }
     }
@@ -654,7 +659,7 @@ hipError_t launch_attend(const AttendPlan &p, const AttendBank &b, const float *
         return e;
     hipLaunchKernelGGL(attend_join_kernel, dim3(b.B), dim3(256), 0, s, a.ml, a.o, p.n_chunks,
                        p.n_lt, 16 * p.ct, b.B, M, b.queries, (int)at_query_bytes(p.dtype, b.d),
-                       p.dtype != AT_F32, (double)b.c, b.c_exact() / b.c, q_hat, l_hat, lse);
+                       p.dtype != AT_F32, b.c, b.c_exact(), q_hat, l_hat, lse);
     return hipGetLastError();
 }
 
