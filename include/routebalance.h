@@ -382,7 +382,10 @@ rb_status rb_route_batch_noalloc(const void *queries, const void *bank, const fl
  * accumulation): one is off by about (|q|^2 + |x|^2) * 2^-23, and a weight by a
  * factor of e to beta times that. rb_attend subtracts the largest score before
  * beta multiplies: the nearest row's weight is the largest, and a number, at any
- * beta. Arguments shared by the calls:
+ * beta. rb_attend_usage and rb_attend_backward recompute weights from lse, which 32
+ * bits hold to |lse| * 2^-24: they follow the formulas while beta * (|q|^2 + |x|^2)
+ * is far below 2^23; past that a weight is between 0 and 1 (in the gradients 2) and
+ * 0 for all but the nearest rows, but says no more. Arguments shared by the calls:
  *   queries   [B][d] of dtype (bf16 for RB_Q4), 16-byte aligned.
  *   bank      RB_F32, RB_BF16: [N][d]; RB_Q4: [N][d/2] bytes (rb_bank_pack);
  *             16-byte aligned.

@@ -47,6 +47,14 @@ __device__ __forceinline__ double lost_to_rounding(float lse, float lse2, double
                : more * (double)lse2 - ((double)lse * 1.4426950408889634 - (double)lse2);
 }
 
+// A weight from its logarithm, c * a - lse2: 1 at most, also where the roundings of a
+// and lse (at most 2^-23 of c * a, each) pass 1 and the difference is of no more use.
+// NaN stays NaN.
+__device__ __forceinline__ float weight_of(float log2w)
+{
+    return __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(log2w, 0.f));
+}
+
 template <int QDT>
 __device__ __forceinline__ void make_side(const PrepArgs &A, int b, int lane)
 {
@@ -66,9 +74,10 @@ __device__ __forceinline__ void make_side(const PrepArgs &A, int b, int lane)
     const bool alive = lse != -INFINITY;
     const float lse2 = alive ? lse * LOG2E : INFINITY;
     // (the gradients are linear in the weights, and get what rounding lost with the
-    // outputs' ones; for the usage it goes into hq)
+    // outputs' ones, by a factor of 2 at most: past that all roundings are as large;
+    // for the usage it goes into hq)
     const double lost = lost_to_rounding(lse, lse2, A.more);
-    const float f = __builtin_amdgcn_exp2f((float)lost);
+    const float f = __builtin_amdgcn_exp2f(__builtin_amdgcn_fmed3f((float)lost, -1.f, 1.f));
     double dot = 0.0;
     if (A.dout) {
         // (a dead request's outputs are no numbers, and its gradients may be none)
@@ -233,8 +242,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_kernel(const UsageAr
             for (int g = 0; g < NG; ++g)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    sum += __builtin_amdgcn_exp2f(
-                        fmaf(c, (acc[r][g][e] + nh) + hq[g][e], -lse2[g][e]));
+                    sum += weight_of(fmaf(c, (acc[r][g][e] + nh) + hq[g][e], -lse2[g][e]));
             sum = rows_reduce(sum, [](float x, float y) { return x + y; });
             if (masked && mk[r] == 0)
                 sum = 0.f;
@@ -296,8 +304,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_gemm_kernel(const Us
                 const float nh = -0.5f * side->norms[128 * wr + 16 * r + col];
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    sum[r] += __builtin_amdgcn_exp2f(
-                        fmaf(c, (acc[r][g][e] + nh) + hq[e], -lse2[e]));
+                    sum[r] += weight_of(fmaf(c, (acc[r][g][e] + nh) + hq[e], -lse2[e]));
             }
         }
 #pragma unroll
@@ -426,7 +433,7 @@ __device__ __forceinline__ void ds_row_tile(const DsArgs &A, const RowTile &T, c
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float a = live ? (sc[g][e] + nh) + hq[e] : 0.f;
-            const float p = live ? __builtin_amdgcn_exp2f(fmaf(c, a, -lse2[e])) : 0.f;
+            const float p = live ? weight_of(fmaf(c, a, -lse2[e])) : 0.f;
             ds[e] = p * dp[g][e];
             sc[g][e] = p;
             sum_db[g][e] = fmaf(2.f * a, ds[e], sum_db[g][e]);   // -distance = 2 a

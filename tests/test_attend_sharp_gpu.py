@@ -13,7 +13,7 @@ import pytest
 import torch
 
 import attend_ref as ref
-from test_attend_gpu import DEV, forward
+from test_attend_gpu import DEV, backward, forward, make
 
 pytestmark = pytest.mark.gpu
 
@@ -72,3 +72,92 @@ def test_all_weight_on_the_nearest(dtype, B, N, beta):
     # rounded once; the logarithm of the ties to a few roundings of itself
     ref.check("lse", out["lse"], lse, U * lse.abs() + 4.0 * U * (1.0 + torch.log(ties[:, 0])),
               f"{dtype} {beta}")
+
+
+def use_of(s, beta, out, decay=0.5):
+    import paper_2606_17949_amd as rb
+    use = torch.ones(s["norms"].shape[0], device=DEV)
+    rb.rb_attend_usage(s["queries"], s["bank"], s["norms"], beta, out["lse"], use, decay=decay,
+                       scales=s["scales"], row_mask=s["mask"])
+    return use
+
+
+@pytest.mark.parametrize("beta", BETAS)
+@pytest.mark.parametrize("B,N", BATCHES)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "q4"])
+def test_requests_that_are_rows(dtype, B, N, beta):
+    """Distance 0: lse is the logarithm of the ties, which 32 bits hold at any beta,
+    and so usage and gradients are exact but for their own roundings."""
+    s = whole(dtype, B, N, seed=N + 1, same=B)
+    out = forward(s, beta)
+    use = use_of(s, beta, out)
+    p = s["near"] / s["near"].sum(1, keepdim=True)
+    # 1/ties from its logarithm (rounded, and a power of two of it), B terms
+    ref.check("usage", use, 0.5 + p.sum(0), (B + 16.0) * U * (0.5 + p.sum(0)), dtype)
+    if dtype == "q4":
+        return
+    got = backward(s, beta, out)
+    torch.cuda.synchronize()
+    for k, v in got.items():
+        assert torch.isfinite(v).all(), k
+    for k, d in (("d_qual", s["dq_hat"].double()), ("d_len", s["dl_hat"].double())):
+        size = p.t() @ d.abs()
+        ref.check(k, got[k], p.t() @ d, (B + 16.0) * U * size + ref.T, dtype)
+    # rows at distance 0 pull nothing: what is left is the rounding of sums of ds
+    # times the row or the request (bf16: ds of 17 bits), times 2 beta
+    assert (got["d_beta"] == 0).all()
+    v = torch.cat((s["qual"], s["len"]), 1).double()
+    do = torch.cat((s["dq_hat"], s["dl_hat"]), 1).double()
+    size = (do.abs() @ v.abs().t() + (p * (do.abs() @ v.abs().t())).sum(1, keepdim=True) +
+            s["dlse"].double().abs()[:, None]) * p
+    for k, e in (("d_queries", size.sum(1)), ("d_bank", size.sum(0))):
+        b = 2.0 * float(np.float32(beta))
+        bound = b * (2.0 ** -16 + (B + 16.0) * U) * e
+        assert (got[k].double().abs() <= bound[:, None]).all(), k
+
+
+@pytest.mark.parametrize("beta", BETAS)
+@pytest.mark.parametrize("B,N", BATCHES)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "q4"])
+def test_weights_recomputed_from_lse_stay_small(dtype, B, N, beta):
+    """Far requests: lse = -beta * distance is rounded to 32 bits, by more than 1 from
+    beta * distance = 2^24 on. Weights recomputed from it are then of no use, but 1 at
+    most (gradients: 2), and 0 for all but the nearest rows."""
+    s = whole(dtype, B, N, seed=N + 2)
+    assert float(s["least"].min()) >= 1.0
+    out = forward(s, beta)
+    use = use_of(s, beta, out, decay=0.0)
+    torch.cuda.synchronize()
+    near = s["near"].sum(0)
+    assert (use >= 0).all() and (use.double() <= near * (1 + 1e-5)).all()
+    if dtype == "q4":
+        return
+    got = backward(s, beta, out)
+    torch.cuda.synchronize()
+    for k, v in got.items():
+        assert torch.isfinite(v).all(), k
+    for k, d in (("d_qual", s["dq_hat"].double()), ("d_len", s["dl_hat"].double())):
+        assert (got[k].double().abs() <= 2.0 * (1 + 1e-5) * (s["near"].t() @ d.abs())).all(), k
+    far = near == 0
+    assert torch.count_nonzero(got["d_bank"][far]) == 0
+
+
+@pytest.mark.parametrize("B,N", [(9, 400), (300, 20_011)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "q4"])
+@pytest.mark.parametrize("beta,scale", [(1e3, 1.0), (1.0, 100.0), (1e-30, 1.0), (1e-3, 1e-3)])
+def test_far_and_flat_usage_and_gradients(dtype, B, N, beta, scale):
+    s = make(dtype, B, N, 128, 4, scale=scale)
+    label = f"{dtype} B={B} beta={beta} scale={scale}"
+    out = forward(s, beta)
+    old = torch.ones(N, device=DEV)
+    value, bound = ref.usage(s["queries"], s["x"], beta, out["lse"], old, 0.5)
+    print("usage", ref.check("usage", use_of(s, beta, out), value, bound, label), flush=True)
+    if dtype == "q4":
+        return
+    got = backward(s, beta, out)
+    torch.cuda.synchronize()
+    want = ref.backward(s["queries"], s["x"], beta, s["qual"], s["len"], out["q_hat"],
+                        out["l_hat"], out["lse"], s["dq_hat"], s["dl_hat"], s["dlse"])
+    for k, (value, bound) in want.items():
+        half = torch.finfo(got[k].dtype).eps / 2
+        print(k, ref.check(k, got[k], value, bound + half * value.abs() + ref.T, label), flush=True)
