@@ -587,7 +587,7 @@ bool plan_attend(int B, int N, int d, int dtype, int M, int n_cu, AttendPlan *p)
     const int ks = at_ks(dtype);
     p->dtype = dtype;
     p->nks = (d + ks - 1) / ks;
-    p->gemm = at_gemm(dtype, B, N, d, n_cu);
+    p->gemm = at_gemm(dtype, B, N, d, M, n_cu);
     if (p->gemm) {
         p->nks = (d + AG_K - 1) / AG_K;
         p->ct = 1;

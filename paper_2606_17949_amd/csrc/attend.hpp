@@ -46,10 +46,19 @@ struct AttendPlan {
 // the compute units. Forward, scan / tiles: 256 x 100,000 x 768 97 / 67 us, 512 x
 // 100,000 x 384 95 / 83, but 128 x 100,000 x 768 59 / 67 and 150 x 15,000 x 768 30 /
 // 40.
-inline bool at_gemm(int dtype, int B, int N, int d, int n_cu)
+// With labels of M models (0: none are averaged) each product of tiles takes 16 of
+// the 2 M label columns, each scan 32: not where that makes twice as many products,
+// unless LDS holds fewer than 64 requests of a scan. 256 x 100,000 x 768, M = 8 90 /
+// 65, 9 107 / 115, 16 102 / 115, 17 180 / 146, 32 176 / 191; 256 x 1,000,000 x 768, M = 8
+// 829 / 507, 9 924 / 887, 16 887 / 891, 32 1,584 / 1,701; 300 x 200,000 x 2,048, M = 16
+// 938 / 717, 32 1,896 / 1,348.
+inline bool at_gemm(int dtype, int B, int N, int d, int M, int n_cu)
 {
     const long tiles = ((long)N + 255) / 256 * ((B + 255) / 256);
-    return dtype == 1 && d >= 128 && B > 128 && 2 * tiles >= n_cu;
+    const bool held = (size_t)((d + 31) / 32) * 64 * 64 <= (size_t)AT_LDS;
+    const int products = (2 * M + 15) / 16, scans = (2 * M + 31) / 32;
+    return dtype == AT_BF16 && d >= 128 && B > 128 && 2 * tiles >= n_cu &&
+           (products < 2 * scans || !held || M == 0);
 }
 
 // Groups of 16 requests of a scan's tile: four where LDS holds them, fewer for a

@@ -1409,7 +1409,7 @@ bool plan_usage(int B, int N, int d, int dtype, int n_cu, UsagePlan *p)
     const int ks = at_ks(dtype);
     p->dtype = dtype;
     p->nks = (d + ks - 1) / ks;
-    p->gemm = at_gemm(dtype, B, N, d, n_cu);
+    p->gemm = at_gemm(dtype, B, N, d, 0, n_cu);
     p->off_side = 0;
     p->off_part = p->gemm ? up256((size_t)B * sizeof(Side)) : 0;
     const size_t group = (size_t)p->nks * ks * (dtype == AT_F32 ? 4 : 2) * 16 + 16 * sizeof(Side);
