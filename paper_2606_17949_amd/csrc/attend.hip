@@ -592,7 +592,6 @@ bool plan_attend(int B, int N, int d, int dtype, int M, int n_cu, AttendPlan *p)
         p->nks = (d + AG_K - 1) / AG_K;
         p->ct = 1;
         p->n_lt = (2 * M + 15) / 16;
-        p->ng = 16;
         p->n_qt = (B + AG_REQS - 1) / AG_REQS;
         p->slabs = (int)(((long)N + AG_ROWS - 1) / AG_ROWS);
         const int most = n_cu / (p->n_qt * p->n_lt);

@@ -459,7 +459,6 @@ __device__ __forceinline__ void ds_row_tile(const DsArgs &A, const RowTile &T, c
         }
     }
     __builtin_amdgcn_sched_barrier(0);
-    const bool any = T.q0 < A.b.B;
     // ---- fragments of ds: [row tile][block of requests][hi, lo][64]
     if (A.ds) {
         constexpr int H = DT == AT_BF16 ? 2 : 1;   // values, and groups of a block
@@ -486,14 +485,13 @@ __device__ __forceinline__ void ds_row_tile(const DsArgs &A, const RowTile &T, c
             }
         }
         rs = rows_reduce(rs, [](float x, float y) { return x + y; });
-        buffer_store4(wave_rsrc(A.rowsum + (any ? (size_t)T.t * A.part_rows : 0) + T.tile16 * 16,
-                                any ? 64u : 0u),
+        buffer_store4(wave_rsrc(A.rowsum + (size_t)T.t * A.part_rows + T.tile16 * 16, 64u),
                       jg == 0 ? (uint32_t)col * 4u : OFF_NONE, rs);
     }
     // ---- the labels' gradient: 16 columns x 16 rows, 4 requests a step
     if (A.d_qual || A.d_len) {
-        const size_t at = ((size_t)(any ? T.t : 0) * A.b.N + T.row0) * M;
-        const uint32_t bytes = any ? (uint32_t)(T.rows * M) * 4u : 0u;
+        const size_t at = ((size_t)T.t * A.b.N + T.row0) * M;
+        const uint32_t bytes = (uint32_t)(T.rows * M) * 4u;
         const __amdgpu_buffer_rsrc_t to_q =
             wave_rsrc((A.d_qual ? A.d_qual : A.d_len) + at, A.d_qual ? bytes : 0u);
         const __amdgpu_buffer_rsrc_t to_l =
