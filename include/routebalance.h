@@ -419,7 +419,9 @@ rb_status rb_route_batch_noalloc(const void *queries, const void *bank, const fl
  *   numbers: one that is NaN makes its model's predictions NaN, an infinite one
  *   infinite (NaN where a weight falls below 1e-38 of the largest, or where both
  *   infinities meet).
- * Sums, maxima and weights are fp32. */
+ * Sums and maxima are fp32, and so are the weights, but where bf16 batches of more
+ * than 128 requests go by as products of tiles: there they enter the averages, and
+ * the sum that divides these, as two bf16 values (17 bits). */
 rb_status rb_attend_workspace_size(int B, int N, int d, rb_dtype dtype, int M, size_t *bytes);
 rb_status rb_attend(const void *queries, const void *bank, const uint8_t *scales,
                     const float *bank_norms, rb_dtype dtype, int B, int N, int d, float beta,

@@ -47,10 +47,11 @@ struct AttendArgs {
 //            MFMA (fp32, 16 label columns x 16 requests, 4 rows): its operand
 //            p[row 4*(lane/16) + e][request lane%16] is register e of the
 //            scores as it stands.
-// Bound by the bank's way from memory (64 requests over 100,000 x 768 bf16 35 us,
-// 4.4 TB/s; over 1,000,000 x 768 in 4 bits 138 us, 3.2 TB/s, where the products and
-// the widening of the codes take as long), small banks by latency (one request over
-// 14,919 x 384 fp32 9.4 us, and 4.3 the join). A second product of fp32 keeps the
+// Bound by the bank's way to the compute units (64 requests over 100,000 x 768 bf16
+// 35 us, 4.4 TB/s, called again and again, so that the last-level cache serves part of
+// it; over 1,000,000 x 768 in 4 bits 133 us a call, 3.3 TB/s, where the products and the
+// widening of the codes take as long), small banks by latency (one request over
+// 14,919 x 384 fp32 9.4 us, and 4.2 the join). A second product of fp32 keeps the
 // weights' 24 bits.
 template <int DT, int NG, int RT, int CT>
 __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const AttendArgs A)
@@ -234,7 +235,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void attend_kernel(const Attend
 // eight fp32 ones that take twice as long each. The sum of the weights is that
 // of hi + lo, a column of ones: it stands behind the labels (ONES false: at
 // column 2 M), or, where they fill all 16 columns, is two products more.
-// 256 requests over 1,000,000 x 768: 500 us, 790 TFLOP/s (the product alone 400, the
+// 256 requests over 1,000,000 x 768: 495 us, 795 TFLOP/s (the product alone 400, the
 // rest powers of two and splits that its waves do all at one time).
 constexpr int ONE2 = 0x3f803f80;   // two bf16 ones
 

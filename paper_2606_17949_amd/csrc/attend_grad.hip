@@ -259,7 +259,7 @@ __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_kernel(const UsageAr
 
 // The same as a matrix product of tiles, for large bf16 batches; part [4 *
 // n_qt][N], one of the waves of each 64 requests. 256 requests over 1,000,000 x 768:
-// 443 us, 890 TFLOP/s.
+// 445 us, 885 TFLOP/s.
 __global__ __launch_bounds__(AT_WAVES * WAVE, 1) void usage_gemm_kernel(const UsageArgs A)
 {
     extern __shared__ __align__(16) uint8_t smem[];
@@ -890,8 +890,9 @@ template <int DT, int NI, int G> struct DqLayout {
 // read across (ds_read_b64_tr_b16: four rows of 16 columns become a column's four
 // rows per lane) for the product over rows: D[column 4*(lane/16) + e][request
 // lane % 16]. With many requests these reads bound it: a slab takes NI + 2 * G of 1
-// KB a wave for 2 * G * NI MFMAs; with few, the rows' way from memory. (256 x 100,000 x 768 with NI = 4 107 us, with 8 87, and 7 more for the
-// join of twice the shares.) Masked rows hold anything and are not fetched: zeros.
+// KB a wave for 2 * G * NI MFMAs; with few, the rows' way from memory. (256 x 100,000 x
+// 768 with NI = 4 107 us, with 8 87, and 7 more for the join of twice the shares.)
+// Masked rows hold anything and are not fetched: zeros.
 template <int DT, int NI, int G>
 __global__ __launch_bounds__(512, 1) void dq_kernel(const DqArgs A)
 {

@@ -36,7 +36,7 @@ inline __host__ __device__ uint32_t at_query_bytes(int dtype, int d)
 // 64 rows; with 32, LDS reads alone take as long as the products.
 constexpr int at_rt(int dt, int ng) { return dt != AT_F32 && ng == 4 ? 4 : 2; }
 // k-steps of bank rows in flight (4-bit rows: 128 elements each; 64 requests over
-// 1,000,000 x 768 of them 148 us with one, 156 with two and spilled registers)
+// 1,000,000 x 768 of them 133 us a call with one, 134 with two and spilled registers)
 constexpr int at_ring(int dt, int rt) { return dt == AT_Q4 ? (rt == 4 ? 1 : 3) : rt == 4 ? 2 : 4; }
 
 // Shares of a bank whose waves' parts stay under 1 GB (32-bit offsets).
@@ -184,8 +184,8 @@ __device__ __forceinline__ void scan_slabs(const AttendBank &A, int nks, const i
     // A block's products are summed by themselves: a score is then a sum of few
     // partial sums, and off by what those few additions round away. (One chain of
     // 256 products of four fp32 elements: 12 requests over 1,473 x 1,024 at beta 21
-    // had gradients off by 2e-5 in their weights, now 3e-6. 64 requests' tiles have
-    // no registers for it.)
+    // had gradients off by 2e-5 in their weights, now 3e-6. Tiles of 64 bf16 requests
+    // have no registers for it: one chain over the row.)
     constexpr bool PARTS = RT == 2;
     f32x4 acc[RT][NG], sum[PARTS ? RT : 1][PARTS ? NG : 1];
     auto clear = [&](auto &x) {
