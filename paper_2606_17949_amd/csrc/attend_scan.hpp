@@ -184,8 +184,8 @@ __device__ __forceinline__ void scan_slabs(const AttendBank &A, int nks, const i
     // A block's products are summed by themselves: a score is then a sum of few
     // partial sums, and off by what those few additions round away. (One chain of
     // 256 products of four fp32 elements: 12 requests over 1,473 x 1,024 at beta 21
-    // had gradients off by 2e-5 in their weights, now 3e-6. Tiles of 64 bf16 requests
-    // have no registers for it: one chain over the row.)
+    // had gradients off by 2e-5 in their weights, now 3e-6. Tiles of 64 requests over
+    // bf16 or 4-bit rows have no registers for it: one chain over the row.)
     constexpr bool PARTS = RT == 2;
     f32x4 acc[RT][NG], sum[PARTS ? RT : 1][PARTS ? NG : 1];
     auto clear = [&](auto &x) {
